@@ -474,6 +474,126 @@ hga_status_t hga_attend_gathered_bwd(const hga_config_t* cfg, const void* Q, hga
                                      void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * A paged cache of keys and values (generation and dense read-out over the
+ * contexts of many sequences, Sec. 4.6; Sec. 2.2: the history's K/V is what
+ * long contexts pay memory for). Position t of sequence s lies in slot t %
+ * page_size of page page_table[s][t / page_size]. Caller-owned device buffers:
+ *   k, v        page p's slot r of kv head h at p * page + r * token + h * head
+ *               elements (strides ks / vs, in elements of the format; 16-byte
+ *               aligned rows; any order of the axes). Page and head strides
+ *               below 2^32 bytes, token strides below 2^27 bytes.
+ *   k_scale, v_scale  HGA_CACHE_E4M3: uint8 [n_pages][Hkv][page_size]; else unused.
+ *   page_table  int32 [n_seqs][table_cap]. An entry outside [0, n_pages) is an
+ *               absent page, as is a position outside the table: rows written
+ *               there are dropped, rows read from there are zeros, and attention
+ *               leaves its positions out. Pages may be shared by sequences.
+ *   page_size   a power of two in [16, 65536].
+ * Formats:
+ *   HGA_CACHE_SAME  rows in cfg->dtype, copied;
+ *   HGA_CACHE_E4M3  rows in 8 bits (OCP e4m3: 3 bits of mantissa, largest value
+ *               448): of a row x of d elements the scale is 2^e, e the least
+ *               integer >= -100 with max |x_j| <= 448 * 2^e over the finite x_j,
+ *               held as the byte e + 127; the codes are x_j / 2^e, an exact
+ *               quotient, rounded to nearest even: x_j is held within 2^-4
+ *               relative, or within 2^(e-10) where it is below 2^(e-6). NaN and
+ *               infinities are held as NaN. A held value is exact in bf16.
+ *
+ * The calls below take the rows of a ragged batch: rows [seq_rows[s],
+ * seq_rows[s + 1]) of n_rows belong to sequence s and are its positions
+ * q_begin[s], q_begin[s] + 1, ... (seq_rows int32 [n_seqs + 1], ascending;
+ * q_begin int32 [n_seqs]; both in device memory, so a captured call follows
+ * them). A sequence may have no rows. Rows before seq_rows[0] and from
+ * seq_rows[n_seqs] on are of no sequence: they are not read, and outputs are left
+ * as they were there.
+ */
+typedef enum { HGA_CACHE_SAME = 0, HGA_CACHE_E4M3 = 1 } hga_cache_format_t;
+
+typedef struct {
+  int64_t page;
+  int64_t token;
+  int64_t head;
+} hga_page_strides_t;
+
+typedef struct {
+  void* k;
+  void* v;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  hga_page_strides_t ks;
+  hga_page_strides_t vs;
+  const int32_t* page_table;
+  int64_t table_cap;
+  int64_t n_pages;
+  int32_t n_seqs;
+  int32_t page_size;
+  hga_cache_format_t format;
+} hga_paged_cache_t;
+
+/*
+ * hga_cache_write - the rows' K and V (cfg->dtype, strides ks / vs, rows
+ * [0, n_rows)) into their pages, in the cache's format. Two rows of one call
+ * that lie in the same slot of the same page leave either.
+ */
+hga_status_t hga_cache_write(const hga_config_t* cfg, const hga_paged_cache_t* cache,
+                             const void* K, hga_strides_t ks, const void* V, hga_strides_t vs,
+                             int64_t n_rows, const int32_t* seq_rows, const int32_t* q_begin,
+                             void* stream);
+
+/*
+ * hga_cache_read - the cached rows of those positions into K and V
+ * (cfg->dtype, strides ks / vs), zeros where the page is absent. Rounds
+ * nothing: a held value is exact in cfg->dtype.
+ */
+hga_status_t hga_cache_read(const hga_config_t* cfg, const hga_paged_cache_t* cache,
+                            void* K, hga_strides_t ks, void* V, hga_strides_t vs,
+                            int64_t n_rows, const int32_t* seq_rows, const int32_t* q_begin,
+                            void* stream);
+
+/*
+ * hga_gather_paged - hga_gather_routed (Sec. 2.1 item 3) with the K/V rows of
+ * sequence `seq` read from the cache: the routed path over a paged, 8-bit
+ * history. Kc, Vc, r_cap and the order of the rows as there;
+ * hga_attend_gathered_fwd and hga_attend_gathered_bwd read them. Rows of absent
+ * pages are zeros.
+ */
+hga_status_t hga_gather_paged(const hga_config_t* cfg, const hga_paged_cache_t* cache, int64_t seq,
+                              int64_t q_begin, int64_t n_q,
+                              const int32_t* sel_groups, const int32_t* n_sel_groups,
+                              void* Kc, void* Vc, int64_t r_cap, void* stream);
+
+/*
+ * hga_attend_paged_fwd - dense causal attention of each sequence's rows over
+ * its cached context: a row at position p attends every position t <= p whose
+ * page is present, its own and the batch's earlier rows among them (written by
+ * hga_cache_write before). One call serves decode steps (one row per sequence),
+ * chunks of a prompt, and both in one batch. Keys after a row never enter its
+ * result, infinities and NaN among them.
+ *
+ *   Q          rows [0, n_rows) of cfg->dtype, strides qs.
+ *   O          rows [0, n_rows) of cfg->dtype, strides os (bf16 rounded to nearest even).
+ *   lse        float32 [n_rows][Hq], natural log. A row with nothing to attend
+ *              has O = 0 and lse = -inf.
+ *   max_rows   the most rows that a sequence of the call has, as far as the caller
+ *              knows (n_rows always will do; at least 1). It chooses the kernels and is no
+ *              limit: a sequence with more rows is computed all the same.
+ *   workspace  device scratch of hga_paged_workspace_size(cfg, n_rows, max_rows)
+ *              bytes; needs no initialisation.
+ * Scores, softmax and accumulation in float32; with bf16 inputs P is rounded
+ * to bf16 before P.V. The keys of a row are split where that fills the GPU and
+ * joined in their order, without atomics: the same call gives the same bits. How they
+ * are split depends on the batch, so a row's last float32 bits do.
+ */
+hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache_t* cache,
+                                  const void* Q, hga_strides_t qs,
+                                  int64_t n_rows, const int32_t* seq_rows, const int32_t* q_begin,
+                                  int64_t max_rows, void* O, hga_strides_t os, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace hga_attend_paged_fwd needs; 0 for an invalid
+ * configuration or count. */
+size_t hga_paged_workspace_size(const hga_config_t* cfg, int64_t n_rows, int64_t max_rows);
+
+/*
  * hga_attend_bwd_noalloc - hga_attend_bwd for callers that cannot allocate
  * device memory (code under HIP graph capture, tight serving loops, harnesses
  * that forbid hipMalloc): the same computation and results, with the

@@ -55,6 +55,7 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 // row's byte offset is one 32 x 32 -> 64-bit product in the kernels.
 constexpr int64_t kMaxTokens = (int64_t)1 << 31;
 constexpr int64_t kMaxStrideBytes = (int64_t)1 << 32;
+constexpr int64_t kMaxTokenBytes = (int64_t)1 << 27;  // token stride inside a cache page
 
 hga_status_t check_tensor(const void* p, hga_strides_t s, int eb) {
   if (!p || !aligned16(p)) return HGA_ERR_INVALID_ARG;
@@ -806,6 +807,159 @@ hga_status_t hga_attend_gathered_bwd(const hga_config_t* cfg, const void* Q, hga
   const hga_strides_t cs = {cfg->head_dim, cfg->head_dim};
   return attend_bwd_impl(cfg, Q, qs, Kc, cs, Vc, cs, O, os, o_f32, dO, dos, lse, q_begin, n_q, grad_begin,
                          sel_groups, n_sel_groups, dQ, dK, dV, workspace, workspace_bytes, stream, &pre, r_cap);
+}
+
+static hga_status_t paged_args(const hga_config_t* cfg, const hga_paged_cache_t* c, hga::PagedArgs* out) {
+  if (!c || !c->k || !c->v || !c->page_table || !aligned16(c->k) || !aligned16(c->v)) return HGA_ERR_INVALID_ARG;
+  if (c->format != HGA_CACHE_SAME && c->format != HGA_CACHE_E4M3) return HGA_ERR_INVALID_ARG;
+  const bool e4m3 = c->format == HGA_CACHE_E4M3;
+  if (e4m3 && (!c->k_scale || !c->v_scale)) return HGA_ERR_INVALID_ARG;
+  if (c->n_seqs < 1 || c->table_cap < 1 || c->n_pages < 1) return HGA_ERR_INVALID_ARG;
+  if (c->table_cap > kMaxTokens || c->n_pages >= kMaxTokens) return HGA_ERR_UNSUPPORTED;
+  if (c->page_size < 1) return HGA_ERR_INVALID_ARG;
+  if (c->page_size < 16 || c->page_size > 65536 || log2_exact(c->page_size) < 0) return HGA_ERR_UNSUPPORTED;
+  const int eb = e4m3 ? 1 : elem_bytes(cfg);
+  const hga_page_strides_t st[2] = {c->ks, c->vs};
+  for (const hga_page_strides_t& x : st) {
+    // a wave's load covers up to 16 rows of a page with one 32-bit offset
+    if (x.page <= 0 || x.token <= 0 || x.head <= 0) return HGA_ERR_INVALID_ARG;
+    if (x.page >= kMaxStrideBytes / eb || x.head >= kMaxStrideBytes / eb || x.token >= kMaxTokenBytes / eb)
+      return HGA_ERR_INVALID_ARG;
+    if (x.page * eb % 16 != 0 || x.token * eb % 16 != 0 || x.head * eb % 16 != 0) return HGA_ERR_INVALID_ARG;
+  }
+  hga::PagedArgs a = {};
+  a.k = static_cast<char*>(c->k); a.v = static_cast<char*>(c->v);
+  a.k_scale = c->k_scale; a.v_scale = c->v_scale;
+  a.k_page = c->ks.page * eb; a.k_tok = c->ks.token * eb; a.k_head = c->ks.head * eb;
+  a.v_page = c->vs.page * eb; a.v_tok = c->vs.token * eb; a.v_head = c->vs.head * eb;
+  a.table = c->page_table; a.table_cap = c->table_cap;
+  a.n_pages = (int)c->n_pages; a.page_shift = log2_exact(c->page_size);
+  a.n_seqs = c->n_seqs; a.n_kv_heads = cfg->n_kv_heads;
+  *out = a;
+  return HGA_OK;
+}
+
+static hga_status_t batch_args(int64_t n_rows, const int32_t* seq_rows, const int32_t* q_begin, hga::PagedArgs* a) {
+  if (n_rows < 1 || n_rows >= kMaxTokens || !seq_rows || !q_begin) return HGA_ERR_INVALID_ARG;
+  a->seq_rows = seq_rows; a->q_begin = q_begin; a->n_rows = n_rows;
+  return HGA_OK;
+}
+
+static hga::DenseRows dense_rows(const void* K, hga_strides_t ks, const void* V, hga_strides_t vs, int eb) {
+  return {static_cast<char*>(const_cast<void*>(K)), static_cast<char*>(const_cast<void*>(V)), ks.token * eb,
+          ks.head * eb, vs.token * eb, vs.head * eb};
+}
+
+hga_status_t hga_cache_write(const hga_config_t* cfg, const hga_paged_cache_t* cache, const void* K, hga_strides_t ks,
+                             const void* V, hga_strides_t vs, int64_t n_rows, const int32_t* seq_rows,
+                             const int32_t* q_begin, void* stream) {
+  HGA_TRY(check_cfg(cfg));
+  hga::PagedArgs a;
+  HGA_TRY(paged_args(cfg, cache, &a));
+  HGA_TRY(batch_args(n_rows, seq_rows, q_begin, &a));
+  const int eb = elem_bytes(cfg);
+  HGA_TRY(check_tensor(K, ks, eb));
+  HGA_TRY(check_tensor(V, vs, eb));
+  if (hga::launch_cache_write(a, dense_rows(K, ks, V, vs, eb), cache->format == HGA_CACHE_E4M3, cfg->dtype == HGA_BF16,
+                              cfg->head_dim, (hipStream_t)stream) != hipSuccess)
+    return HGA_ERR_HIP;
+  return HGA_OK;
+}
+
+hga_status_t hga_cache_read(const hga_config_t* cfg, const hga_paged_cache_t* cache, void* K, hga_strides_t ks, void* V,
+                            hga_strides_t vs, int64_t n_rows, const int32_t* seq_rows, const int32_t* q_begin,
+                            void* stream) {
+  HGA_TRY(check_cfg(cfg));
+  hga::PagedArgs a;
+  HGA_TRY(paged_args(cfg, cache, &a));
+  HGA_TRY(batch_args(n_rows, seq_rows, q_begin, &a));
+  const int eb = elem_bytes(cfg);
+  HGA_TRY(check_tensor(K, ks, eb));
+  HGA_TRY(check_tensor(V, vs, eb));
+  if (hga::launch_cache_read(a, dense_rows(K, ks, V, vs, eb), cache->format == HGA_CACHE_E4M3, cfg->dtype == HGA_BF16,
+                             cfg->head_dim, (hipStream_t)stream) != hipSuccess)
+    return HGA_ERR_HIP;
+  return HGA_OK;
+}
+
+hga_status_t hga_gather_paged(const hga_config_t* cfg, const hga_paged_cache_t* cache, int64_t seq, int64_t q_begin,
+                              int64_t n_q, const int32_t* sel_groups, const int32_t* n_sel_groups, void* Kc, void* Vc,
+                              int64_t r_cap, void* stream) {
+  HGA_TRY(check_cfg(cfg));
+  hga::PagedArgs p;
+  HGA_TRY(paged_args(cfg, cache, &p));
+  HGA_TRY(check_rows(q_begin, n_q));
+  if (seq < 0 || seq >= cache->n_seqs) return HGA_ERR_INVALID_ARG;
+  if (!n_sel_groups || (cfg->top_groups > 0 && !sel_groups)) return HGA_ERR_INVALID_ARG;
+  if (!Kc || !Vc || !aligned16(Kc) || !aligned16(Vc)) return HGA_ERR_INVALID_ARG;
+  if (r_cap % kChunk != 0 || r_cap < min_r_cap(cfg)) return HGA_ERR_INVALID_ARG;
+  AttnArgs a = attn_args(cfg, nullptr, hga_strides_t{1, 1}, nullptr, hga_strides_t{1, 1}, nullptr,
+                         hga_strides_t{1, 1}, q_begin, n_q, sel_groups, n_sel_groups);
+  a.r_cap = r_cap;
+  if (hga::launch_gather_paged(a, p, (int)seq, Kc, Vc, cache->format == HGA_CACHE_E4M3, cfg->dtype == HGA_BF16,
+                               cfg->head_dim, (hipStream_t)stream) != hipSuccess)
+    return HGA_ERR_HIP;
+  return HGA_OK;
+}
+
+// Folded rows (row, query head of a kv head) of a partial result's slot, and a form's scratch.
+static int64_t slot_rows(const hga_config_t* c, int64_t n_rows, int m_rows) {
+  const int64_t f = n_rows * (c->n_q_heads / c->n_kv_heads);
+  return f < m_rows ? f : m_rows;
+}
+static size_t paged_ws(const hga_config_t* c, int64_t n_rows, int m_rows) {
+  const size_t rows = 2 * (size_t)hga::kPagedWorkgroups * slot_rows(c, n_rows, m_rows);
+  return hga::kPagedWorkgroups * sizeof(int4) + rows * (c->head_dim + 2) * sizeof(float);
+}
+// Whether no sequence is expected to have more rows than the form for few takes at a time.
+static bool only_few(const hga_config_t* c, int64_t max_rows) {
+  return max_rows <= hga::kPagedFewRows / (c->n_q_heads / c->n_kv_heads);
+}
+
+size_t hga_paged_workspace_size(const hga_config_t* cfg, int64_t n_rows, int64_t max_rows) {
+  if (check_cfg(cfg) != HGA_OK || n_rows < 1 || n_rows >= kMaxTokens || max_rows < 1) return 0;
+  return paged_ws(cfg, n_rows, only_few(cfg, max_rows) ? hga::kPagedFewRows : hga::kPagedTileRows);
+}
+
+hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache_t* cache, const void* Q,
+                                  hga_strides_t qs, int64_t n_rows, const int32_t* seq_rows, const int32_t* q_begin,
+                                  int64_t max_rows, void* O, hga_strides_t os, float* lse, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  HGA_TRY(check_cfg(cfg));
+  hga::PagedAttnArgs a = {};
+  HGA_TRY(paged_args(cfg, cache, &a.p));
+  HGA_TRY(batch_args(n_rows, seq_rows, q_begin, &a.p));
+  const int eb = elem_bytes(cfg);
+  HGA_TRY(check_tensor(Q, qs, eb));
+  HGA_TRY(check_tensor(O, os, eb));
+  if (!lse || max_rows < 1) return HGA_ERR_INVALID_ARG;
+  if (!workspace || !aligned16(workspace) || workspace_bytes < hga_paged_workspace_size(cfg, n_rows, max_rows))
+    return HGA_ERR_WORKSPACE;
+  const int G = cfg->n_q_heads / cfg->n_kv_heads;
+  a.Q = static_cast<const char*>(Q); a.q_tok = qs.token * eb; a.q_head = qs.head * eb;
+  a.O = static_cast<char*>(O); a.o_tok = os.token * eb; a.o_head = os.head * eb;
+  a.lse = lse;
+  a.n_q_heads = cfg->n_q_heads; a.gqa_shift = log2_exact(G);
+  a.scale_log2 = eff_scale(cfg) * 1.4426950408889634f;
+  a.info = static_cast<int4*>(workspace);
+  a.part = reinterpret_cast<float*>(a.info + hga::kPagedWorkgroups);
+  const bool e4m3 = cache->format == HGA_CACHE_E4M3, bf16 = cfg->dtype == HGA_BF16;
+  // Each form takes the sequences whose rows suit it; the two share the
+  // workspace, one after the other on the stream. A single sequence, and a call
+  // of few rows, needs one form only, which then takes whatever there is.
+  const int few_rows = hga::kPagedFewRows / G;
+  const bool few = only_few(cfg, max_rows), both = !few && cache->n_seqs > 1;
+  for (int form = 0; form < 2; ++form) {
+    const bool is_few = form == 0;
+    if (!both && is_few != few) continue;
+    a.min_rows = both && !is_few ? few_rows + 1 : 1;
+    a.max_rows = both && is_few ? few_rows : 0x7fffffff;
+    a.slot_rows = (int)slot_rows(cfg, n_rows, is_few ? hga::kPagedFewRows : hga::kPagedTileRows);
+    a.part_ml = a.part + 2 * (int64_t)hga::kPagedWorkgroups * a.slot_rows * cfg->head_dim;
+    if (hga::launch_attend_paged(a, is_few, e4m3, bf16, cfg->head_dim, (hipStream_t)stream) != hipSuccess)
+      return HGA_ERR_HIP;
+  }
+  return HGA_OK;
 }
 
 }  // extern "C"

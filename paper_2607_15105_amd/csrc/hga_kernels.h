@@ -118,6 +118,47 @@ struct TierArgs {
   int64_t hist_end;
 };
 
+// A paged cache and the rows of a ragged batch over it: row r of sequence s
+// (seq_rows[s] <= r < seq_rows[s + 1]) is position q_begin[s] + r - seq_rows[s].
+struct PagedArgs {
+  char* k;                   // position t of kv head h: page * k_page + (t & mask) * k_tok + h * k_head bytes
+  char* v;
+  uint8_t* k_scale;          // e4m3: [n_pages][Hkv][page size], exponent + 127; else null
+  uint8_t* v_scale;
+  int64_t k_page, k_tok, k_head, v_page, v_tok, v_head;  // bytes
+  const int32_t* table;      // [n_seqs][table_cap]
+  int64_t table_cap;
+  int n_pages, page_shift, n_seqs, n_kv_heads;
+  const int32_t* seq_rows;   // [n_seqs + 1]
+  const int32_t* q_begin;    // [n_seqs]
+  int64_t n_rows;
+};
+
+// Dense K/V rows of the call (cache_write's input, cache_read's output).
+struct DenseRows {
+  char* k;
+  char* v;
+  int64_t k_tok, k_head, v_tok, v_head;  // bytes
+};
+
+// Attention of the batch's rows over the cache. Rows of a sequence and kv head
+// are folded with the G query heads: folded row f is row f / G, head f % G.
+struct PagedAttnArgs {
+  PagedArgs p;
+  const char* Q;
+  int64_t q_tok, q_head;     // bytes
+  char* O;
+  int64_t o_tok, o_head;     // bytes
+  float* lse;                // [n_rows][Hq]
+  int n_q_heads, gqa_shift;
+  int min_rows, max_rows;    // sequences with min_rows <= rows <= max_rows are this launch's
+  int slot_rows;             // folded rows of a partial result's slot
+  int4* info;                // [workgroups]: the item that a workgroup leaves unfinished
+  float* part;               // [workgroups][2][slot_rows][D], then [workgroups][2][slot_rows][2] (max, sum)
+  float* part_ml;
+  float scale_log2;
+};
+
 // Summary tables, float32 [Hkv][d/4][cap][4]: float offset of quad q (elements
 // 4q..4q+3) of row r of kv head h.
 __host__ __device__ inline int64_t quad_off(int h, int q, int64_t r, int d, int64_t cap) {
@@ -167,5 +208,21 @@ constexpr int kRowsBwdMaxRows = 4096;
 constexpr int kRowsDkvKeys = 16;  // keys per workgroup of the per-query dK/dV kernel
 constexpr int kRowsRouteRound = 4096;  // candidate chunks a one-row routing workgroup scores per round
 hipError_t launch_attend_rows_bwd(const AttnArgs& a, int64_t n_rows, bool bf16, int head_dim, hipStream_t s);
+
+// Paged cache. `e4m3`: rows held in 8 bits, else in the element type.
+hipError_t launch_cache_write(const PagedArgs& a, const DenseRows& d, bool e4m3, bool bf16, int head_dim, hipStream_t s);
+hipError_t launch_cache_read(const PagedArgs& a, const DenseRows& d, bool e4m3, bool bf16, int head_dim, hipStream_t s);
+// The routed rows of sequence `seq`'s query blocks into compact rows (a: the
+// routing, as launch_gather's; p.seq_rows / q_begin unused).
+hipError_t launch_gather_paged(const AttnArgs& a, const PagedArgs& p, int seq, void* kc, void* vc, bool e4m3, bool bf16,
+                               int head_dim, hipStream_t s);
+// Attention over the cache in two forms, each followed by the joining of the
+// results that two or more workgroups share. `few`: at most kPagedFewRows
+// folded rows at a time, waves on different keys; else kPagedTileRows folded
+// rows at a time, waves on different rows.
+constexpr int kPagedFewRows = 32;
+constexpr int kPagedTileRows = 256;
+constexpr int kPagedWorkgroups = 256;  // one per CU
+hipError_t launch_attend_paged(const PagedAttnArgs& a, bool few, bool e4m3, bool bf16, int head_dim, hipStream_t s);
 
 }  // namespace hga

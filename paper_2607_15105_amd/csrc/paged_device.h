@@ -1,0 +1,106 @@
+// Device code of the paged key/value cache: where a position's rows lie, the
+// 8-bit format, and the rows of a ragged batch.
+//
+// A cached row (one token, one kv head, K or V) is held either in the
+// configuration's element type or in 8 bits: e4m3 codes and one power-of-two
+// scale, code * 2^e with e the least integer >= kMinExp under which the row's
+// largest finite magnitude is at most 448 * 2^e. x * 2^-e is exact, so a code
+// is one rounding away from its value, and code * 2^e has four significant
+// bits: it is exact in bf16, and reading back rounds nothing. (A scale of
+// amax / 448 would round three times for a gain of less than one binade of
+// range, which a floating format does not need.)
+#pragma once
+#include "hga_device.h"
+#include "hga_kernels.h"
+
+namespace hga {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kMinExp = -100;  // 2^(kMinExp - 9), a code's least step, is normal in bf16 and float32
+
+// Exponent of a row whose largest finite magnitude is `amax` (>= 0).
+__device__ inline int row_exponent(float amax) {
+  // 448 = 1.75 * 2^8: carry into the exponent field when the mantissa is over .75
+  const int k = (int)((__float_as_uint(amax) + 0x1fffffu) >> 23) - 127 - 8;
+  return k < kMinExp ? kMinExp : k;
+}
+__device__ inline float exp2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
+
+// Codes of x[0..3] * inv (inv = 2^-e) in one word; what is not finite becomes NaN.
+__device__ inline uint32_t codes4(const float* x, float inv) {
+  float y[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) y[j] = fabsf(x[j]) < __builtin_inff() ? x[j] * inv : __builtin_nanf("");
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  return (uint32_t)w;
+}
+
+// 16 bytes of T from the codes that hold them: eight codes for bf16, four for float.
+template <typename T> struct Codes;
+template <> struct Codes<__bf16> {
+  static constexpr int kWords = 2;
+  __device__ static inline uint4 decode(const uint32_t* w, float scale) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], scale, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], scale, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], scale, true);
+    return make_uint4(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b),
+                      __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d));
+  }
+};
+template <> struct Codes<float> {
+  static constexpr int kWords = 1;
+  __device__ static inline uint4 decode(const uint32_t* w, float scale) {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[0], false);
+    const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[0], true);
+    return make_uint4(__float_as_uint(a[0] * scale), __float_as_uint(a[1] * scale), __float_as_uint(b[0] * scale),
+                      __float_as_uint(b[1] * scale));
+  }
+};
+
+// Page of position t (any value) of sequence s, -1 if it is absent: outside the
+// table, or an entry outside [0, n_pages).
+__device__ inline int page_of(const PagedArgs& a, int s, int64_t t) {
+  if (t < 0 || (t >> a.page_shift) >= a.table_cap) return -1;
+  const int p = a.table[(int64_t)s * a.table_cap + (t >> a.page_shift)];
+  return (uint32_t)p < (uint32_t)a.n_pages ? p : -1;
+}
+
+// Byte offset of slot `slot` of page `page` (page and token strides below 4 GB).
+__device__ inline uint64_t page_off(int page, int slot, int64_t page_b, int64_t tok_b) {
+  return (uint64_t)(uint32_t)page * (uint32_t)page_b + (uint64_t)(uint32_t)slot * (uint32_t)tok_b;
+}
+// Index of the scale byte of (page, kv head, slot).
+__device__ inline int64_t scale_off(const PagedArgs& a, int page, int h, int slot) {
+  return (((int64_t)page * a.n_kv_heads + h) << a.page_shift) + slot;
+}
+
+// Rows of sequence s: [first, first + n) within the call's rows, n >= 0 whatever seq_rows holds.
+__device__ inline void rows_of(const PagedArgs& a, int s, int& first, int& n) {
+  const int b = a.seq_rows[s], e = a.seq_rows[s + 1], last = (int)a.n_rows;
+  first = b < 0 ? 0 : (b > last ? last : b);
+  n = (e > last ? last : e) - first;
+  if (n < 0 || b < 0) n = 0;
+}
+
+// Sequence and position of the call's rows r0 + i, i < NR (the same r0 in the
+// whole wave): 64 entries of seq_rows at a time, counted by ballot, so that
+// any number of sequences costs independent loads and no search. seq[i] is -1
+// for a row of no sequence.
+template <int NR>
+__device__ inline void find_rows(const PagedArgs& a, int64_t r0, int lane, int (&seq)[NR]) {
+  int cnt[NR] = {};
+  for (int base = 0; base <= a.n_seqs; base += 64) {
+    const int v = base + lane <= a.n_seqs ? a.seq_rows[base + lane] : 0x7fffffff;
+#pragma unroll
+    for (int i = 0; i < NR; ++i) cnt[i] += __popcll(__ballot((int64_t)v <= r0 + i));
+  }
+#pragma unroll
+  for (int i = 0; i < NR; ++i) seq[i] = r0 + i < a.n_rows && cnt[i] >= 1 && cnt[i] <= a.n_seqs ? cnt[i] - 1 : -1;
+}
+
+}  // namespace hga

@@ -19,6 +19,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhga.so"
 _lib = None
 
 HGA_F32, HGA_BF16 = 0, 1
+CACHE_SAME, CACHE_E4M3 = 0, 1
 OP_ROUTE, OP_BWD = 0, 1
 NOALLOC_SCRATCH_BYTES = 48 << 20  # HGA_NOALLOC_SCRATCH_BYTES
 STATUS = {0: "ok", -1: "invalid argument", -2: "unsupported configuration",
@@ -51,6 +52,19 @@ class GroupCache(ctypes.Structure):
 class Strides(ctypes.Structure):
     """hga_strides_t (element strides; head_dim axis contiguous)."""
     _fields_ = [("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class PageStrides(ctypes.Structure):
+    """hga_page_strides_t (element strides; head_dim axis contiguous)."""
+    _fields_ = [("page", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class PagedCacheDesc(ctypes.Structure):
+    """hga_paged_cache_t: device buffers of a paged key/value cache."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("ks", PageStrides), ("vs", PageStrides),
+                ("page_table", ctypes.c_void_p), ("table_cap", ctypes.c_int64), ("n_pages", ctypes.c_int64),
+                ("n_seqs", ctypes.c_int32), ("page_size", ctypes.c_int32), ("format", ctypes.c_int32)]
 
 
 def library_path() -> str:
@@ -93,6 +107,13 @@ def lib() -> ctypes.CDLL:
                                               P, P, P, P, P, P, SZ, P]
         L.hga_gather_routed.argtypes = [C, P, S, P, S, I64, I64, P, P, P, P, I64, P]
         L.hga_attend_gathered_fwd.argtypes = [C, P, S, P, P, I64, I64, I64, P, P, S, P, P, P]
+        PC = ctypes.POINTER(PagedCacheDesc)
+        for fn in ("hga_cache_write", "hga_cache_read"):
+            getattr(L, fn).argtypes = [C, PC, P, S, P, S, I64, P, P, P]
+        L.hga_gather_paged.argtypes = [C, PC, I64, I64, I64, P, P, P, P, I64, P]
+        L.hga_attend_paged_fwd.argtypes = [C, PC, P, S, I64, P, P, I64, P, S, P, P, SZ, P]
+        L.hga_paged_workspace_size.argtypes = [C, I64, I64]
+        L.hga_paged_workspace_size.restype = SZ
         L.hga_workspace_size.argtypes = [C, ctypes.c_int, I64, I64, I64]
         L.hga_workspace_size.restype = SZ
         L.hga_status_string.argtypes = [ctypes.c_int]
@@ -101,7 +122,8 @@ def lib() -> ctypes.CDLL:
                    "hga_attend_bwd", "hga_attend_bwd_noalloc", "hga_gather_routed",
                    "hga_attend_gathered_fwd", "hga_route_rows", "hga_attend_rows_fwd",
                    "hga_attend_rows_bwd", "hga_group_cache_clear", "hga_route_cached",
-                   "hga_group_cache_update", "hga_gather_tiered", "hga_attend_gathered_bwd"):
+                   "hga_group_cache_update", "hga_gather_tiered", "hga_attend_gathered_bwd",
+                   "hga_cache_write", "hga_cache_read", "hga_gather_paged", "hga_attend_paged_fwd"):
             getattr(L, fn).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -423,6 +445,150 @@ def attend_gathered_bwd(cfg: Config, Q, Kc, Vc, K_act, V_act, act_begin: int, O,
         _strides(K_act), act_begin, _ptr(O), _strides(O), _ptr(o_f32), _ptr(dO), _strides(dO), _ptr(lse),
         q_begin, Q.shape[0], grad_begin, _ptr(sel_groups), _ptr(n_sel_groups), _ptr(dQ), _ptr(dK), _ptr(dV),
         _ptr(workspace), workspace.numel(), _stream())
+
+
+# ---------------------------------------------------------------------------
+# Paged key/value cache of many sequences, optionally in 8 bits
+# ---------------------------------------------------------------------------
+
+@dataclass
+class PagedCache:
+    """Device buffers of a paged cache and their descriptor. k, v:
+    [n_pages, page_size, Hkv, d] views (any order in memory with d contiguous);
+    k_scale, v_scale: uint8 [n_pages, Hkv, page_size] of an e4m3 cache."""
+    k: torch.Tensor
+    v: torch.Tensor
+    page_table: torch.Tensor
+    k_scale: torch.Tensor | None
+    v_scale: torch.Tensor | None
+    desc: PagedCacheDesc
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _torch_dtype(cfg: Config):
+    return torch.bfloat16 if cfg.dtype == HGA_BF16 else torch.float32
+
+
+def paged_cache(cfg: Config, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor,
+                k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None) -> PagedCache:
+    """A cache over the given buffers: k, v [n_pages, page_size, Hkv, d] of the
+    configuration's dtype, or of 8 bits (float8_e4m3fn, uint8) with scales;
+    page_table int32 [n_seqs, table_cap]. The buffers stay the caller's."""
+    _need(k.dim() == 4 and k.shape == v.shape and tuple(k.shape[2:]) == (cfg.n_kv_heads, cfg.head_dim),
+          "k, v: [n_pages, page_size, Hkv, d] tensors of one shape")
+    _need(k.stride(3) == 1 and v.stride(3) == 1, "k, v: contiguous head_dim")
+    _need(k.dtype == v.dtype and k.dtype in (_torch_dtype(cfg), torch.float8_e4m3fn, torch.uint8),
+          "k, v: the configuration's dtype, float8_e4m3fn or uint8")
+    _need(page_table.dim() == 2 and page_table.dtype == torch.int32 and page_table.is_contiguous(),
+          "page_table: a dense int32 [n_seqs, table_cap] tensor")
+    e4m3 = k.element_size() == 1
+    if e4m3:
+        for t in (k_scale, v_scale):
+            _need(t is not None and t.dtype == torch.uint8 and t.is_contiguous()
+                  and tuple(t.shape) == (k.shape[0], cfg.n_kv_heads, k.shape[1]),
+                  "k_scale, v_scale: dense uint8 [n_pages, Hkv, page_size] tensors")
+    else:
+        _need(k_scale is None and v_scale is None, "scales belong to an 8-bit cache")
+    _need(len({t.device for t in (k, v, page_table, k_scale, v_scale) if t is not None}) == 1,
+          "the cache's buffers lie on one device")
+    desc = PagedCacheDesc(k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale), PageStrides(*k.stride()[:3]),
+                          PageStrides(*v.stride()[:3]), page_table.data_ptr(), page_table.shape[1], k.shape[0],
+                          page_table.shape[0], k.shape[1], CACHE_E4M3 if e4m3 else CACHE_SAME)
+    return PagedCache(k, v, page_table, k_scale, v_scale, desc)
+
+
+def alloc_paged_cache(cfg: Config, n_seqs: int, table_cap: int, n_pages: int, page_size: int = 64, e4m3: bool = False,
+                      device="cuda") -> PagedCache:
+    """A cache of n_pages empty pages and a page table of absent pages, a head's
+    tokens side by side within a page."""
+    shape = (n_pages, cfg.n_kv_heads, page_size, cfg.head_dim)
+    dt = torch.float8_e4m3fn if e4m3 else _torch_dtype(cfg)
+    k, v = (torch.zeros(shape, dtype=dt, device=device).transpose(1, 2) for _ in range(2))
+    ks, vs = (torch.zeros(shape[:3], dtype=torch.uint8, device=device) if e4m3 else None for _ in range(2))
+    return paged_cache(cfg, k, v, torch.full((n_seqs, table_cap), -1, dtype=torch.int32, device=device), ks, vs)
+
+
+def _check_batch(cfg: Config, cache: PagedCache, seq_rows: torch.Tensor, q_begin: torch.Tensor, heads: int,
+                 *rows: torch.Tensor) -> None:
+    """The arguments of a call over a ragged batch: what the kernels would
+    otherwise read out of bounds, and the device that they run on."""
+    n_seqs = cache.desc.n_seqs
+    _need(seq_rows.dtype == q_begin.dtype == torch.int32 and seq_rows.is_contiguous() and q_begin.is_contiguous()
+          and tuple(seq_rows.shape) == (n_seqs + 1,) and tuple(q_begin.shape) == (n_seqs,),
+          "seq_rows [n_seqs + 1], q_begin [n_seqs]: dense int32 tensors")
+    shape, dt = (rows[0].shape[0], heads, cfg.head_dim), _torch_dtype(cfg)
+    for t in rows:
+        _need(tuple(t.shape) == shape and t.dtype == dt, f"rows: [n_rows, {heads}, {cfg.head_dim}] tensors of {dt}")
+    dev = cache.k.device
+    _need(all(t.device == dev for t in (seq_rows, q_begin, *rows)), "all tensors lie on the cache's device")
+    _on_current(dev)
+
+
+def _on_current(dev: torch.device) -> None:
+    _need(dev.type == "cuda", "expected GPU tensors")
+    _need(dev.index == torch.cuda.current_device(), "the tensors' device is not the current one")
+
+
+def cache_write(cfg: Config, cache: PagedCache, K: torch.Tensor, V: torch.Tensor, seq_rows: torch.Tensor,
+                q_begin: torch.Tensor) -> None:
+    """Rows seq_rows[s] .. seq_rows[s + 1] - 1 of K, V [n_rows, Hkv, d] into
+    positions q_begin[s] ... of sequence s, in the cache's format."""
+    _check_batch(cfg, cache, seq_rows, q_begin, cfg.n_kv_heads, K, V)
+    _call("hga_cache_write",
+        ctypes.byref(cfg), ctypes.byref(cache.desc), _ptr(K), _strides(K), _ptr(V), _strides(V), K.shape[0],
+        _ptr(seq_rows), _ptr(q_begin), _stream())
+
+
+def cache_read(cfg: Config, cache: PagedCache, K: torch.Tensor, V: torch.Tensor, seq_rows: torch.Tensor,
+               q_begin: torch.Tensor) -> None:
+    """The cached rows of those positions into K, V [n_rows, Hkv, d]; zeros
+    where the page is absent."""
+    _check_batch(cfg, cache, seq_rows, q_begin, cfg.n_kv_heads, K, V)
+    _call("hga_cache_read",
+        ctypes.byref(cfg), ctypes.byref(cache.desc), _ptr(K), _strides(K), _ptr(V), _strides(V), K.shape[0],
+        _ptr(seq_rows), _ptr(q_begin), _stream())
+
+
+def gather_paged(cfg: Config, cache: PagedCache, seq: int, q_begin: int, n_q: int, sel_groups: torch.Tensor,
+                 n_sel_groups: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor) -> None:
+    """gather_routed with the rows of cached sequence `seq`."""
+    _need(Kc.shape == Vc.shape and Kc.dim() == 4 and Kc.is_contiguous() and Vc.is_contiguous()
+          and Kc.dtype == Vc.dtype == _torch_dtype(cfg)
+          and (Kc.shape[0], Kc.shape[1], Kc.shape[3]) == (n_q // cfg.query_block, cfg.n_kv_heads, cfg.head_dim),
+          "Kc, Vc: dense [n_q/B, Hkv, r_cap, d] tensors of one shape")
+    _need(all(t.dtype == torch.int32 and t.is_contiguous() for t in (sel_groups, n_sel_groups))
+          and n_sel_groups.numel() == Kc.shape[0] * Kc.shape[1]
+          and sel_groups.numel() == n_sel_groups.numel() * max(cfg.top_groups, 1),
+          "sel_groups [n_q/B, Hkv, top_groups], n_sel_groups [n_q/B, Hkv]: dense int32 tensors")
+    dev = cache.k.device
+    _need(all(t.device == dev for t in (sel_groups, n_sel_groups, Kc, Vc)), "all tensors lie on the cache's device")
+    _on_current(dev)
+    _call("hga_gather_paged",
+        ctypes.byref(cfg), ctypes.byref(cache.desc), seq, q_begin, n_q, _ptr(sel_groups), _ptr(n_sel_groups), _ptr(Kc),
+        _ptr(Vc), Kc.shape[2], _stream())
+
+
+def paged_workspace_size(cfg: Config, n_rows: int, max_rows: int | None = None) -> int:
+    return int(lib().hga_paged_workspace_size(ctypes.byref(cfg), n_rows, n_rows if max_rows is None else max_rows))
+
+
+def attend_paged_fwd(cfg: Config, cache: PagedCache, Q: torch.Tensor, seq_rows: torch.Tensor, q_begin: torch.Tensor,
+                     O: torch.Tensor, lse: torch.Tensor, workspace: torch.Tensor, max_rows: int | None = None) -> None:
+    """Dense causal attention of the rows of Q [n_rows, Hq, d] over their
+    sequences' cached positions up to their own. max_rows: the most rows that a
+    sequence of the call has (default: n_rows)."""
+    _check_batch(cfg, cache, seq_rows, q_begin, cfg.n_q_heads, Q, O)
+    _need(tuple(lse.shape) == (Q.shape[0], cfg.n_q_heads) and lse.dtype == torch.float32 and lse.is_contiguous()
+          and lse.device == Q.device == workspace.device,
+          "lse: a dense float32 [n_rows, Hq] tensor on the cache's device, as the workspace")
+    _call("hga_attend_paged_fwd",
+        ctypes.byref(cfg), ctypes.byref(cache.desc), _ptr(Q), _strides(Q), Q.shape[0], _ptr(seq_rows), _ptr(q_begin),
+        Q.shape[0] if max_rows is None else max_rows, _ptr(O), _strides(O), _ptr(lse), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream())
 
 
 # ---------------------------------------------------------------------------

@@ -1,0 +1,139 @@
+"""The paged cache's refusals, without a GPU: invalid calls return (or raise in
+the binding) before anything is launched; and the float64 oracle of its 8-bit
+format against torch's own conversion."""
+
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2607_15105_amd import hga
+from tests import paged_oracle as po
+
+FAKE = 0x10000  # a 16-byte aligned non-null address; never dereferenced on these paths
+
+
+def _cfg(**kw):
+    return hga.make_config(kw.pop("hq", 8), kw.pop("hkv", 2), kw.pop("d", 128), **kw)
+
+
+def _desc(**kw):
+    st = hga.PageStrides(2 * 64 * 128, 128, 64 * 128)
+    base = dict(k=FAKE, v=FAKE, k_scale=None, v_scale=None, ks=st, vs=st, page_table=FAKE, table_cap=16, n_pages=32,
+                n_seqs=4, page_size=64, format=hga.CACHE_SAME)
+    base.update(kw)
+    return hga.PagedCacheDesc(*base.values())
+
+
+def _attend(c=None, desc=None, n_rows=8, max_rows=8, q=FAKE, qs=None, o=FAKE, lse=FAKE, ws=FAKE, size=None, rows=FAKE,
+            begin=FAKE):
+    c = c or _cfg()
+    S = qs or hga.Strides(8 * 128, 128)
+    # one byte short unless told otherwise: a call that is right up to there is told so, and launches nothing
+    size = max(int(hga.paged_workspace_size(c, n_rows, max_rows)) - 1, 0) if size is None else size
+    return hga.lib().hga_attend_paged_fwd(ctypes.byref(c), ctypes.byref(desc or _desc()), q, S, n_rows, rows, begin,
+                                          max_rows, o, S, lse, ws, size, None)
+
+
+def test_descriptor_refusals():
+    ok = -3  # everything right but the workspace
+    assert _attend() == ok
+    bad = lambda **kw: _attend(desc=_desc(**kw))
+    for name in ("k", "v", "page_table"):
+        assert bad(**{name: 0}) == -1, name
+    assert bad(k=FAKE + 8) == -1
+    assert bad(format=hga.CACHE_E4M3) == -1                       # no scales
+    assert bad(format=hga.CACHE_E4M3, k_scale=FAKE, v_scale=FAKE) == ok
+    assert bad(format=hga.CACHE_E4M3, k_scale=FAKE) == -1
+    for name in ("n_seqs", "table_cap", "n_pages", "page_size"):
+        assert bad(**{name: 0}) == -1 and bad(**{name: -1}) == -1, name
+    assert bad(n_pages=1 << 31) == -2 and bad(table_cap=(1 << 31) + 1) == -2
+    for size in (1, 8, 24, 48, 131072):
+        assert bad(page_size=size) == -2, size
+    for size in (16, 65536):
+        assert bad(page_size=size) == ok, size
+    st = lambda *a: hga.PageStrides(*a)
+    assert bad(ks=st(0, 128, 8192)) == -1 and bad(vs=st(16384, -128, 8192)) == -1 and bad(vs=st(16384, 128, 0)) == -1
+    assert bad(ks=st(16384, 132, 8192)) == -1                     # rows not 16-byte aligned
+    assert bad(ks=st(1 << 31, 128, 8192)) == -1                   # 4 GB
+    assert bad(ks=st(16384, 1 << 26, 8192)) == -1 and bad(ks=st(16384, (1 << 26) - 8, 8192)) == ok
+    assert bad(vs=st(16384, 128, 1 << 31)) == -1
+    assert bad(vs=st((1 << 62) + 8, 128, 8192)) == -1             # whose bytes would wrap
+
+
+def test_attention_refusals():
+    assert _attend(n_rows=0) == -1 and _attend(n_rows=-1) == -1 and _attend(n_rows=1 << 31) == -1
+    assert _attend(max_rows=0) == -1
+    assert _attend(q=0) == -1 and _attend(o=FAKE + 2) == -1 and _attend(lse=0) == -1
+    assert _attend(rows=0) == -1 and _attend(begin=0) == -1
+    assert _attend(ws=0, size=1 << 40) == -3 and _attend(ws=FAKE + 4, size=1 << 40) == -3
+    assert _attend(qs=hga.Strides(8 * 128 + 4, 128)) == -1
+    assert _attend(_cfg(hq=6, hkv=2)) == -2 and _attend(_cfg(d=96)) == -2
+    assert hga.paged_workspace_size(_cfg(d=96), 4) == 0
+    assert hga.paged_workspace_size(_cfg(), 0, 1) == 0 and hga.paged_workspace_size(_cfg(), 4, 0) == 0
+    # a call of few rows needs less, and the size never shrinks with the rows
+    sizes = [hga.paged_workspace_size(_cfg(), n, 1) for n in (1, 2, 8, 64, 5000)]
+    assert sizes == sorted(sizes) and sizes[-1] <= hga.paged_workspace_size(_cfg(), 5000, 5000)
+
+
+def test_write_read_and_gather_refusals():
+    L, c, S = hga.lib(), _cfg(), hga.Strides(2 * 128, 128)
+    for fn in (L.hga_cache_write, L.hga_cache_read):
+        call = lambda k=FAKE, n=4, rows=FAKE, desc=None, st=S: fn(ctypes.byref(c), ctypes.byref(desc or _desc()), k, st,
+                                                                 FAKE, S, n, rows, FAKE, None)
+        assert call(k=0) == -1 and call(k=FAKE + 4) == -1 and call(n=0) == -1 and call(n=1 << 31) == -1
+        assert call(rows=0) == -1 and call(desc=_desc(page_size=20)) == -2 and call(st=hga.Strides(0, 128)) == -1
+        assert fn(None, ctypes.byref(_desc()), FAKE, S, FAKE, S, 4, FAKE, FAKE, None) == -1
+        assert fn(ctypes.byref(c), None, FAKE, S, FAKE, S, 4, FAKE, FAKE, None) == -1
+    cap = hga.gathered_rows(c)
+    gather = lambda seq=0, q=1024, n=64, r=cap, kc=FAKE: L.hga_gather_paged(ctypes.byref(c), ctypes.byref(_desc()), seq, q,
+                                                                           n, FAKE, FAKE, kc, FAKE, r, None)
+    assert gather(seq=-1) == -1 and gather(seq=4) == -1 and gather(q=1000) == -1 and gather(n=0) == -1
+    assert gather(r=cap - 64) == -1 and gather(r=cap + 1) == -1 and gather(kc=0) == -1
+
+
+def test_binding_refuses_what_the_kernels_would_misread():
+    c = _cfg()
+    k = torch.zeros(4, 64, 2, 128, dtype=torch.bfloat16)
+    table = torch.zeros(3, 5, dtype=torch.int32)
+    cache = hga.paged_cache(c, k, k.clone(), table)
+    assert (cache.desc.n_pages, cache.desc.page_size, cache.desc.n_seqs, cache.desc.table_cap) == (4, 64, 3, 5)
+    assert (cache.desc.ks.page, cache.desc.ks.token, cache.desc.ks.head) == (64 * 256, 256, 128)
+    f8 = k.to(torch.float8_e4m3fn)
+    sc = torch.zeros(4, 2, 64, dtype=torch.uint8)
+    assert hga.paged_cache(c, f8, f8.clone(), table, sc, sc.clone()).desc.format == hga.CACHE_E4M3
+    for args in ((k, k[:2], table), (k[..., :64], k[..., :64], table), (k.float(), k.float(), table),
+                 (k, k, table.long()), (k, k, table[:, :2]), (k, k, table, sc, sc), (f8, f8, table),
+                 (f8, f8, table, sc, sc[:, :, :32]), (k.transpose(2, 3), k.transpose(2, 3), table), (k[0], k[0], table[0])):
+        with pytest.raises(ValueError):
+            hga.paged_cache(c, *args)
+    rows, begin = torch.zeros(4, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    x = torch.zeros(6, 2, 128, dtype=torch.bfloat16)
+    for fn in (hga.cache_write, hga.cache_read):
+        for a in ((x, x, rows, begin),                       # not on a GPU
+                  (x, x[:5], rows, begin), (x.float(), x.float(), rows, begin), (x, x, rows[:3], begin),
+                  (x, x, rows, begin.long()), (x[:, :1], x[:, :1], rows, begin)):
+            with pytest.raises(ValueError):
+                fn(c, cache, *a)
+    q = torch.zeros(6, 8, 128, dtype=torch.bfloat16)
+    ws = torch.zeros(64, dtype=torch.uint8)
+    for a in ((q, rows, begin, q, torch.zeros(6, 8), ws), (q, rows, begin, q[:4], torch.zeros(6, 8), ws),
+              (q, rows, begin, q, torch.zeros(6, 2), ws), (x, rows, begin, x, torch.zeros(6, 2), ws)):
+        with pytest.raises(ValueError):
+            hga.attend_paged_fwd(c, cache, *a)
+
+
+def test_oracle_of_the_format_matches_the_types_own_rounding():
+    """Values that fit without a scale (row maximum 448) are held as
+    torch.float8_e4m3fn holds them; the exponent is the least that fits."""
+    gen = torch.Generator().manual_seed(1)
+    x = torch.randn(50, 128, generator=gen) * torch.exp2(torch.randint(-14, 6, (50, 1), generator=gen).float())
+    x[:, 0] = 448.0
+    val, e = po.held(x)
+    assert bool((e == 0).all()) and torch.equal(val, x.to(torch.float8_e4m3fn).double())
+    y = torch.ones(6, 128)
+    y[:, 0] = torch.tensor([448.0, 449.0, 896.0, 1.75 * 2.0 ** -92, 2.0 ** -120, 3.0e38])
+    y[3:, 1:] = 0
+    assert po.held(y)[1].tolist() == [0, 1, 1, -100, -100, 120]
+    assert math.isnan(float(po.held(torch.tensor([[1.0, math.inf]]))[0][0, 1]))
