@@ -149,29 +149,37 @@ __device__ inline Share take_share(const PagedAttnArgs& a, int wg, int T, int st
 
 // ---------------------------------------------------------------- key tiles
 
-// Pages of a tile's 64 positions, a position per lane: the page (0 where there
-// is none), which are present and before the item's end, and the rows' scales.
+// Pages of a tile's 64 positions, a position per lane. `entry` is the table's
+// entry as loaded, or -1; nothing looks at it before use(), so the load can be
+// under way beside the tile before it. (Loads return in order: a wait for the
+// entry right after it was asked for is a wait for every row asked for before
+// it. With that, 64 ragged contexts took 343 us, 8-bit rows; a 2,048-token chunk at the
+// end of 32K 1,383 us.)
 struct TileKeys {
-  int page;
-  uint64_t ok;
-  float ks, vs;
-};
+  int entry;
+  int page;       // 0 where there is none
+  uint64_t ok;    // positions that are present and before the item's end
+  uint32_t ks, vs;  // the rows' scale bytes
 
-template <bool F8>
-__device__ inline TileKeys find_keys(const PagedArgs& a, int s, int h, int64_t tile, int64_t end, int lane) {
-  const int64_t t = tile * 64 + lane;
-  const int page = t < end ? page_of(a, s, t) : -1;
-  TileKeys k;
-  k.ok = __ballot(page >= 0);
-  k.page = page < 0 ? 0 : page;
-  k.ks = k.vs = 1.0f;
-  if constexpr (F8) {
-    const int64_t o = scale_off(a, k.page, h, (int)(t & ((1 << a.page_shift) - 1)));
-    k.ks = __uint_as_float((uint32_t)a.k_scale[o] << 23);
-    k.vs = __uint_as_float((uint32_t)a.v_scale[o] << 23);
+  __device__ inline void ask(const PagedArgs& a, int s, int64_t tile, int64_t end, int lane) {
+    const int64_t t = tile * 64 + lane, at = t >> a.page_shift;
+    entry = -1;
+    if (t < end && at < a.table_cap) entry = a.table[(int64_t)s * a.table_cap + at];
   }
-  return k;
-}
+  __device__ inline void use(const PagedArgs& a) {
+    const bool there = (uint32_t)entry < (uint32_t)a.n_pages;
+    ok = __ballot(there);
+    page = there ? entry : 0;
+  }
+  template <bool F8>
+  __device__ inline void ask_scales(const PagedArgs& a, int h, int64_t tile, int lane) {
+    if constexpr (F8) {
+      const int64_t o = scale_off(a, page, h, (int)((tile * 64 + lane) & ((1 << a.page_shift) - 1)));
+      ks = a.k_scale[o];
+      vs = a.v_scale[o];
+    }
+  }
+};
 
 template <typename T>
 __device__ inline bool finite16(const uint4& w) {
@@ -241,7 +249,7 @@ struct TileRegs {
       const bool v = j >= NI;
       uint4 out[PE * EB / 16];
       if constexpr (F8) {
-        const float sc = __shfl(v ? k.vs : k.ks, row, 64);
+        const float sc = __uint_as_float((uint32_t)__shfl((int)(v ? k.vs : k.ks), row, 64) << 23);
 #pragma unroll
         for (int o = 0; o < PE * EB / 16; ++o) {
           uint32_t c[Codes<T>::kWords];
@@ -499,10 +507,16 @@ __global__ __launch_bounds__(256) void paged_few_kernel(PagedAttnArgs a) {
     int64_t x = sh.kt + wave;
     TileRegs<T, D, F8, 1> r;
     TileKeys cur, nxt;
+    // the rows of tile y, whose pages are in cur, and the pages of the one after it
+    auto ask = [&](int64_t y) {
+      cur.use(a.p);
+      nxt.ask(a.p, sh.s, y + NW, end, lane);
+      cur.template ask_scales<F8>(a.p, sh.h, y, lane);
+      r.load(a.p, sh.h, y, cur.page, 0, lane);
+    };
     if (x < last) {
-      cur = find_keys<F8>(a.p, sh.s, sh.h, x, end, lane);
-      r.load(a.p, sh.h, x, cur.page, 0, lane);
-      nxt = find_keys<F8>(a.p, sh.s, sh.h, x + NW, end, lane);
+      cur.ask(a.p, sh.s, x, end, lane);
+      ask(x);
     }
     while (x < last) {
       // positions after the first row lie in this tile, or some are not there
@@ -512,8 +526,7 @@ __global__ __launch_bounds__(256) void paged_few_kernel(PagedAttnArgs a) {
       __builtin_amdgcn_wave_barrier();
       if (x + NW < last) {
         cur = nxt;
-        r.load(a.p, sh.h, x + NW, cur.page, 0, lane);
-        nxt = find_keys<F8>(a.p, sh.s, sh.h, x + 2 * NW, end, lane);
+        ask(x + NW);
       }
       w.step(st, x, ok, masked, c, lane);
       if (bad) w.template add_bad<F8>(a.p, sh.s, sh.h, x, bad, lane);
@@ -596,9 +609,15 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs a) {
     const int64_t last = sh.kt + n;
     int64_t x = sh.kt;
     TileRegs<T, D, F8, NW> r;
-    TileKeys cur = find_keys<F8>(a.p, sh.s, sh.h, x, end, lane), nxt;
-    r.load(a.p, sh.h, x, cur.page, wave, lane);
-    nxt = find_keys<F8>(a.p, sh.s, sh.h, x + 1, end, lane);
+    TileKeys cur, nxt;
+    auto ask = [&](int64_t y) {
+      cur.use(a.p);
+      nxt.ask(a.p, sh.s, y + 1, end, lane);
+      cur.template ask_scales<F8>(a.p, sh.h, y, lane);
+      r.load(a.p, sh.h, y, cur.page, wave, lane);
+    };
+    cur.ask(a.p, sh.s, x, end, lane);
+    ask(x);
     auto put = [&](int64_t tile, const TileKeys& k) {
       const bool masked = tile * 64 + 63 > first_pos || k.ok != ~0ull;
       const uint64_t bad = r.store(smem + (tile & 1) * W::STAGE, k, masked, wave, lane);
@@ -608,8 +627,7 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs a) {
     uint64_t ok = cur.ok;
     if (x + 1 < last) {
       cur = nxt;
-      r.load(a.p, sh.h, x + 1, cur.page, wave, lane);
-      nxt = find_keys<F8>(a.p, sh.s, sh.h, x + 2, end, lane);
+      ask(x + 1);
     }
     __syncthreads();
     for (; x < last; ++x) {
@@ -628,8 +646,7 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs a) {
         ok = cur.ok;
         if (x + 2 < last) {
           cur = nxt;
-          r.load(a.p, sh.h, x + 2, cur.page, wave, lane);
-          nxt = find_keys<F8>(a.p, sh.s, sh.h, x + 3, end, lane);
+          ask(x + 2);
         }
       }
       __syncthreads();
