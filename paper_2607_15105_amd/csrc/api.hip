@@ -903,13 +903,13 @@ hga_status_t hga_gather_paged(const hga_config_t* cfg, const hga_paged_cache_t* 
 }
 
 // Folded rows (row, query head of a kv head) of a partial result's slot, and a form's scratch.
-static int64_t slot_rows(const hga_config_t* c, int64_t n_rows, int m_rows) {
-  const int64_t f = n_rows * (c->n_q_heads / c->n_kv_heads);
-  return f < m_rows ? f : m_rows;
+static int64_t slot_rows(const hga_config_t* c, int64_t n_rows, bool few) {
+  const int64_t f = n_rows * (c->n_q_heads / c->n_kv_heads), m = few ? hga::kPagedFewRows : hga::kPagedTileRows;
+  return f < m ? f : m;
 }
-static size_t paged_ws(const hga_config_t* c, int64_t n_rows, int m_rows) {
-  const size_t rows = 2 * (size_t)hga::kPagedWorkgroups * slot_rows(c, n_rows, m_rows);
-  return hga::kPagedWorkgroups * sizeof(int4) + rows * (c->head_dim + 2) * sizeof(float);
+static size_t paged_ws(const hga_config_t* c, int64_t n_rows, bool few) {
+  const size_t rows = 2 * (size_t)hga::paged_workgroups(few) * slot_rows(c, n_rows, few);
+  return hga::paged_workgroups(few) * sizeof(int4) + rows * (c->head_dim + 2) * sizeof(float);
 }
 // Whether no sequence is expected to have more rows than the form for few takes at a time.
 static bool only_few(const hga_config_t* c, int64_t max_rows) {
@@ -918,7 +918,8 @@ static bool only_few(const hga_config_t* c, int64_t max_rows) {
 
 size_t hga_paged_workspace_size(const hga_config_t* cfg, int64_t n_rows, int64_t max_rows) {
   if (check_cfg(cfg) != HGA_OK || n_rows < 1 || n_rows >= kMaxTokens || max_rows < 1) return 0;
-  return paged_ws(cfg, n_rows, only_few(cfg, max_rows) ? hga::kPagedFewRows : hga::kPagedTileRows);
+  const size_t few = paged_ws(cfg, n_rows, true), tile = paged_ws(cfg, n_rows, false);
+  return only_few(cfg, max_rows) || few > tile ? few : tile;
 }
 
 hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache_t* cache, const void* Q,
@@ -942,7 +943,6 @@ hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache
   a.n_q_heads = cfg->n_q_heads; a.gqa_shift = log2_exact(G);
   a.scale_log2 = eff_scale(cfg) * 1.4426950408889634f;
   a.info = static_cast<int4*>(workspace);
-  a.part = reinterpret_cast<float*>(a.info + hga::kPagedWorkgroups);
   const bool e4m3 = cache->format == HGA_CACHE_E4M3, bf16 = cfg->dtype == HGA_BF16;
   // Each form takes the sequences whose rows suit it; the two share the
   // workspace, one after the other on the stream. A single sequence, and a call
@@ -954,8 +954,9 @@ hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache
     if (!both && is_few != few) continue;
     a.min_rows = both && !is_few ? few_rows + 1 : 1;
     a.max_rows = both && is_few ? few_rows : 0x7fffffff;
-    a.slot_rows = (int)slot_rows(cfg, n_rows, is_few ? hga::kPagedFewRows : hga::kPagedTileRows);
-    a.part_ml = a.part + 2 * (int64_t)hga::kPagedWorkgroups * a.slot_rows * cfg->head_dim;
+    a.slot_rows = (int)slot_rows(cfg, n_rows, is_few);
+    a.part = reinterpret_cast<float*>(a.info + hga::paged_workgroups(is_few));
+    a.part_ml = a.part + 2 * (int64_t)hga::paged_workgroups(is_few) * a.slot_rows * cfg->head_dim;
     if (hga::launch_attend_paged(a, is_few, e4m3, bf16, cfg->head_dim, (hipStream_t)stream) != hipSuccess)
       return HGA_ERR_HIP;
   }

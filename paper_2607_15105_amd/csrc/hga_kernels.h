@@ -222,7 +222,10 @@ hipError_t launch_gather_paged(const AttnArgs& a, const PagedArgs& p, int seq, v
 // rows at a time, waves on different rows.
 constexpr int kPagedFewRows = 32;
 constexpr int kPagedTileRows = 256;
-constexpr int kPagedWorkgroups = 256;  // one per CU
+constexpr int kPagedFewKeys = 5, kPagedTileKeys = 6;  // keys of a unit of work, log2
+constexpr int kPagedFewWorkgroups = 512;   // two per CU
+constexpr int kPagedTileWorkgroups = 256;  // one per CU
+inline int paged_workgroups(bool few) { return few ? kPagedFewWorkgroups : kPagedTileWorkgroups; }
 hipError_t launch_attend_paged(const PagedAttnArgs& a, bool few, bool e4m3, bool bf16, int head_dim, hipStream_t s);
 
 }  // namespace hga

@@ -30,6 +30,7 @@ struct SeqShape {
   int first, n;      // rows of the call
   int64_t qb, cap;   // position of the first row; positions that the page table covers
   int T;             // tokens per row tile
+  int ks;            // keys per unit, log2
   bool plain;        // all positions inside [0, cap)
 
   __device__ inline int nt() const { return (n + T - 1) / T; }
@@ -41,18 +42,20 @@ struct SeqShape {
   // at least one, so that rows with nothing to attend are written too
   __device__ inline int64_t tiles(int64_t j) const {
     const int64_t e = end(j);
-    return e > 0 ? (e + 63) >> 6 : 1;
+    return e > 0 ? (e + (1 << ks) - 1) >> ks : 1;
   }
-  // units of the row tiles before j <= nt - 1: sum over i < j of ceil((qb + (i+1) T) / 64)
+  // units of the row tiles before j <= nt - 1: sum over i < j of ceil((qb + (i+1) T) / 2^ks)
   __device__ inline int64_t before(int64_t j) const {
+    if (j == 0) return 0;
     if (!plain) return j * tiles(0);
-    if (T >= 64) return j * ((qb + 63) >> 6) + (T >> 6) * (j * (j + 1) / 2);
-    const int q = 64 / T;  // row tiles in which the sum's terms grow by one
+    const int up = (1 << ks) - 1;
+    if (T > up) return j * ((qb + up) >> ks) + (T >> ks) * (j * (j + 1) / 2);
+    const int q = (1 << ks) / T;  // row tiles in which the sum's terms grow by one
     const int64_t a = j / q;
     const int b = (int)(j % q);
     int64_t period = 0, rest = 0;
     for (int i = 1; i <= q; ++i) {
-      const int64_t term = (qb + 63 + (int64_t)i * T) >> 6;
+      const int64_t term = (qb + up + (int64_t)i * T) >> ks;
       period += term;
       if (i <= b) rest += term;
     }
@@ -61,6 +64,7 @@ struct SeqShape {
   __device__ inline int64_t units() const { return n == 0 ? 0 : before(nt() - 1) + tiles(nt() - 1); }
 };
 
+template <int KS>
 __device__ inline SeqShape shape_of(const PagedAttnArgs& a, int s, int T) {
   SeqShape q;
   rows_of(a.p, s, q.first, q.n);
@@ -69,6 +73,7 @@ __device__ inline SeqShape shape_of(const PagedAttnArgs& a, int s, int T) {
   const int64_t cap = a.p.table_cap << a.p.page_shift;
   q.cap = cap < ((int64_t)1 << 31) ? cap : (int64_t)1 << 31;
   q.T = T;
+  q.ks = KS;
   q.plain = q.qb >= 0 && q.qb + q.n <= q.cap;
   return q;
 }
@@ -81,8 +86,8 @@ struct Share {
   SeqShape q;   // of sequence s
 };
 
-// NT threads; `lds` holds NT / 64 + 2 int64.
-template <int NT>
+// NT threads, W workgroups, units of 2^KS keys; `lds` holds NT / 64 + 2 int64.
+template <int NT, int W, int KS>
 __device__ inline Share take_share(const PagedAttnArgs& a, int wg, int T, int step, int64_t least, int64_t* lds) {
   constexpr int NW = NT / 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -90,7 +95,7 @@ __device__ inline Share take_share(const PagedAttnArgs& a, int wg, int T, int st
   int64_t sum = 0;
   for (int k = 0; k < c; ++k) {
     const int s = tid * c + k;
-    if (s < n_seqs) sum += a.p.n_kv_heads * shape_of(a, s, T).units();
+    if (s < n_seqs) sum += a.p.n_kv_heads * shape_of<KS>(a, s, T).units();
   }
   int64_t inc = sum;
 #pragma unroll
@@ -107,7 +112,7 @@ __device__ inline Share take_share(const PagedAttnArgs& a, int wg, int T, int st
     total += lds[w];
   }
   Share sh;
-  sh.per = (total + kPagedWorkgroups - 1) / kPagedWorkgroups;
+  sh.per = (total + W - 1) / W;
   sh.per = sh.per < least ? least : (sh.per + step - 1) / step * step;
   sh.u0 = wg * sh.per;
   sh.u1 = sh.u0 + sh.per;
@@ -117,7 +122,7 @@ __device__ inline Share take_share(const PagedAttnArgs& a, int wg, int T, int st
   if (sh.u0 < sh.u1 && off >= 0 && off < sum) {  // this thread's sequences hold the first unit
     int s = tid * c;
     for (; s < n_seqs - 1; ++s) {
-      const int64_t m = a.p.n_kv_heads * shape_of(a, s, T).units();
+      const int64_t m = a.p.n_kv_heads * shape_of<KS>(a, s, T).units();
       if (off < m) break;
       off -= m;
     }
@@ -130,7 +135,7 @@ __device__ inline Share take_share(const PagedAttnArgs& a, int wg, int T, int st
   if (sh.u0 < sh.u1) {
     sh.s = __builtin_amdgcn_readfirstlane((int)lds[NW]);
     off = lds[NW + 1];
-    sh.q = shape_of(a, sh.s, T);
+    sh.q = shape_of<KS>(a, sh.s, T);
     const int64_t m = sh.q.units();
     sh.h = __builtin_amdgcn_readfirstlane((int)(off / m));
     off -= sh.h * m;
@@ -149,22 +154,24 @@ __device__ inline Share take_share(const PagedAttnArgs& a, int wg, int T, int st
 
 // ---------------------------------------------------------------- key tiles
 
-// Pages of a tile's 64 positions, a position per lane. `entry` is the table's
+// Pages of a tile's KT positions (32 or 64), a position per lane. `entry` is the table's
 // entry as loaded, or -1; nothing looks at it before use(), so the load can be
 // under way beside the tile before it. (Loads return in order: a wait for the
 // entry right after it was asked for is a wait for every row asked for before
 // it. With that, 64 ragged contexts took 343 us, 8-bit rows; a 2,048-token chunk at the
 // end of 32K 1,383 us.)
+template <int KT>
 struct TileKeys {
+  static constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << KT) - 1;
   int entry;
   int page;       // 0 where there is none
   uint64_t ok;    // positions that are present and before the item's end
   uint32_t ks, vs;  // the rows' scale bytes
 
   __device__ inline void ask(const PagedArgs& a, int s, int64_t tile, int64_t end, int lane) {
-    const int64_t t = tile * 64 + lane, at = t >> a.page_shift;
+    const int64_t t = tile * KT + lane, at = t >> a.page_shift;
     entry = -1;
-    if (t < end && at < a.table_cap) entry = a.table[(int64_t)s * a.table_cap + at];
+    if (lane < KT && t < end && at < a.table_cap) entry = a.table[(int64_t)s * a.table_cap + at];
   }
   __device__ inline void use(const PagedArgs& a) {
     const bool there = (uint32_t)entry < (uint32_t)a.n_pages;
@@ -174,7 +181,7 @@ struct TileKeys {
   template <bool F8>
   __device__ inline void ask_scales(const PagedArgs& a, int h, int64_t tile, int lane) {
     if constexpr (F8) {
-      const int64_t o = scale_off(a, page, h, (int)((tile * 64 + lane) & ((1 << a.page_shift) - 1)));
+      const int64_t o = scale_off(a, page, h, (int)((tile * KT + lane) & ((1 << a.page_shift) - 1)));
       ks = a.k_scale[o];
       vs = a.v_scale[o];
     }
@@ -210,16 +217,29 @@ __device__ inline uint4 only_finite(const uint4& w) {
   return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
-// One wave's share (of NW waves) of a 64-key tile of K and V, in registers. A
+// One LDS stage of a KT-key tile: K rows, then V (rows, or transposed for
+// float32, which has no transposing LDS load).
+template <typename T, int D, int KT>
+struct Stage {
+  using TL = Tile<T, D>;
+  static constexpr bool TR = Elem<T>::kBytes == 2;
+  static constexpr int kV = KT * TL::kRowPitch;  // offset of V
+  static constexpr int kBytes = kV + (TR ? KT * TL::kRowPitch : D * (KT + 1) * 4);
+  // element (d, kpos) of the transposed V
+  __device__ static inline int t_off(int d, int kpos) { return kV + (d * (KT + 1) + kpos) * 4; }
+};
+
+// One wave's share (of NW waves) of a KT-key tile of K and V, in registers. A
 // load instruction covers R whole rows; pages hold 16 tokens or more, so they lie in
 // one page and the address is a scalar plus a fixed lane offset.
-template <typename T, int D, bool F8, int NW>
+template <typename T, int D, int KT, bool F8, int NW>
 struct TileRegs {
   using TL = Tile<T, D>;
+  using ST = Stage<T, D, KT>;
   static constexpr int EB = Elem<T>::kBytes;
   static constexpr int PPR = (F8 ? D : D * EB) / 16;  // 16-byte pieces of a held row
   static constexpr int R = 64 / PPR;
-  static constexpr int NI = PPR;                      // instructions per tensor
+  static constexpr int NI = KT / R;                   // instructions per tensor
   static constexpr int IPW = 2 * NI / NW;
   static constexpr int PE = F8 ? 16 : 16 / EB;        // elements of a piece
   u32x4 w[IPW];
@@ -231,7 +251,7 @@ struct TileRegs {
       const int j = wave * IPW + i, row = (j % NI) * R;
       const bool v = j >= NI;
       const int pg = __builtin_amdgcn_readlane(page, row);
-      const int slot = (int)((tile * 64 + row) & mask);
+      const int slot = (int)((tile * KT + row) & mask);
       const int64_t tok = v ? a.v_tok : a.k_tok;
       const char* base = v ? a.v + page_off(pg, slot, a.v_page, tok) + h * a.v_head
                            : a.k + page_off(pg, slot, a.k_page, tok) + h * a.k_head;
@@ -241,7 +261,7 @@ struct TileRegs {
 
   // Into the LDS stage. masked: rows that are not ok are zeros, and what is not
   // finite in V is left out; returns the rows of V that have such elements.
-  __device__ inline uint64_t store(char* st, const TileKeys& k, bool masked, int wave, int lane) const {
+  __device__ inline uint64_t store(char* st, const TileKeys<KT>& k, bool masked, int wave, int lane) const {
     uint64_t bad = 0;
 #pragma unroll
     for (int i = 0; i < IPW; ++i) {
@@ -282,13 +302,13 @@ struct TileRegs {
       for (int o = 0; o < PE * EB / 16; ++o) {
         const int e = (lane % PPR) * PE + o * 16 / EB;
         if (EB == 2 || !v) {
-          *reinterpret_cast<uint4*>(st + (v ? TL::kRowBytes : 0) + TL::row_off(row, e)) = out[o];
+          *reinterpret_cast<uint4*>(st + (v ? ST::kV : 0) + TL::row_off(row, e)) = out[o];
         } else {
           const uint32_t x[4] = {out[o].x, out[o].y, out[o].z, out[o].w};
           const int kp = kpos_of<Elem<T>::E>(row);
 #pragma unroll
           for (int y = 0; y < 4; ++y)
-            *reinterpret_cast<uint32_t*>(st + TL::kRowBytes + TL::t_off(e + y, kp)) = x[y];
+            *reinterpret_cast<uint32_t*>(st + ST::t_off(e + y, kp)) = x[y];
         }
       }
     }
@@ -298,16 +318,17 @@ struct TileRegs {
 
 // ---------------------------------------------------------------- one wave's rows
 
-// 32 folded rows of one wave: lane l holds (half the head dim of) row l % 32.
-template <typename T, int D>
+// 32 folded rows of one wave, over KT-key tiles: lane l holds (half the head
+// dim of) row l % 32.
+template <typename T, int D, int KT>
 struct WaveRows {
   using EL = Elem<T>;
   using Frag = typename EL::Frag;
   using TL = Tile<T, D>;
   static constexpr int E = EL::E, KS = EL::KSTEP, EB = EL::kBytes;
   static constexpr int NKS = D / KS, NDT = D / 32, VPS = 16 / E;
-  static constexpr bool TR = EB == 2;
-  static constexpr int STAGE = TL::kRowBytes + (TR ? TL::kRowBytes : TL::kTBytes);
+  static constexpr int NH = KT / 32;
+  using ST = Stage<T, D, KT>;
 
   Frag qf[NKS];
   f32x16 oacc[NDT];
@@ -336,25 +357,27 @@ struct WaveRows {
   __device__ __forceinline__ void step(const char* st, int64_t tile, uint64_t ok, bool masked, float c, int lane) {
     const int hh = lane >> 5, l32 = lane & 31;
     const float lazy = 8.0f / c;
-    f32x16 s[2] = {f32x16{}, f32x16{}};
+    f32x16 s[NH];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < NH; ++t) s[t] = f32x16{};
+#pragma unroll
+    for (int t = 0; t < NH; ++t)
 #pragma unroll
       for (int ks = 0; ks < NKS; ++ks) {
         const Frag kf = EL::load_frag(st + TL::row_off(32 * t + l32, ks * KS + E * hh));
         s[t] = EL::mma(kf, qf[ks], s[t]);
       }
     if (masked) {
-      const int64_t rel = pos - tile * 64;  // keys 0 .. rel are at or before the row
+      const int64_t rel = pos - tile * KT;  // keys 0 .. rel are at or before the row
       const uint64_t see = (ok & (rel < 0 ? 0 : rel >= 63 ? ~0ull : (2ull << rel) - 1)) >> (4 * hh);
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < NH; ++t)
 #pragma unroll
         for (int v = 0; v < 16; ++v)
           if (!((see >> (32 * t + 8 * (v >> 2) + (v & 3))) & 1)) s[t][v] = -__builtin_inff();
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < NH; ++t) {
       float mx = -__builtin_inff();
 #pragma unroll
       for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[t][v]);
@@ -386,8 +409,8 @@ struct WaveRows {
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) {
           Frag vf;
-          if constexpr (TR) vf = tr_frag<TL>(st + TL::kRowBytes, 32 * dt, 16 * k + 4 * hh, 16 * k + 8 + 4 * hh, lane);
-          else vf = EL::load_frag(st + TL::kRowBytes + TL::t_off(32 * dt + l32, KS * k + E * hh));
+          if constexpr (ST::TR) vf = tr_frag<TL>(st + ST::kV, 32 * dt, 16 * k + 4 * hh, 16 * k + 8 + 4 * hh, lane);
+          else vf = EL::load_frag(st + ST::t_off(32 * dt + l32, KS * k + E * hh));
           oacc[dt] = EL::mma(vf, pf, oacc[dt]);
         }
       }
@@ -403,7 +426,7 @@ struct WaveRows {
     while (bad) {
       const int kk = __builtin_ctzll(bad);
       bad &= bad - 1;
-      const int64_t t = tile * 64 + kk;
+      const int64_t t = tile * KT + kk;
       const int page = page_of(a, s, t);
       if (page < 0 || pos < t) continue;
       const int slot = (int)(t & ((1 << a.page_shift) - 1));
@@ -445,10 +468,10 @@ __device__ inline float lse_of(float m, float l, float c) {
 
 // The workgroup's place in the concatenation of all units: consecutive shares
 // on one XCD (workgroups are dealt round-robin to the eight), whose L2 then holds what they share.
-__device__ inline int share_index() { return (blockIdx.x & 7) * (kPagedWorkgroups / 8) + (blockIdx.x >> 3); }
+__device__ inline int share_index() { return (blockIdx.x & 7) * (gridDim.x / 8) + (blockIdx.x >> 3); }
 
 // Follows a share item by item: f(s, q, h, j, first tile, tiles, whole) and the record of the one left unfinished.
-template <typename F>
+template <int KS, typename F>
 __device__ inline void walk(const PagedAttnArgs& a, Share sh, int wg, int T, F&& f) {
   int64_t u = sh.u0;
   if (threadIdx.x == 0) a.info[wg] = make_int4(0, 0, 0, 0);
@@ -470,7 +493,7 @@ __device__ inline void walk(const PagedAttnArgs& a, Share sh, int wg, int T, F&&
           sh.h = 0;
           do {
             if (++sh.s >= a.p.n_seqs) return;  // not reached: units remain, so a sequence with rows does
-            sh.q = shape_of(a, sh.s, T);
+            sh.q = shape_of<KS>(a, sh.s, T);
           } while (sh.q.n == 0);
         }
       }
@@ -484,54 +507,59 @@ __device__ inline void walk(const PagedAttnArgs& a, Share sh, int wg, int T, F&&
 
 // Up to 32 folded rows per item: the four waves take every fourth tile each,
 // on the same rows, with LDS of their own and no barrier; their results are
-// joined at the item's end.
+// joined at the item's end. 32-key tiles, so that two workgroups fit a CU and
+// one's rows are under way while the other begins or ends an item. 8-bit rows
+// are asked for two tiles ahead, which keeps as many bytes under way as one of
+// bf16 rows does (16 KB a wave, 128 KB a CU).
 template <typename T, int D, bool F8>
-__global__ __launch_bounds__(256) void paged_few_kernel(PagedAttnArgs a) {
-  using W = WaveRows<T, D>;
-  constexpr int NW = 4, OP = D + 4;
-  static_assert(NW * 32 * OP * 4 <= NW * W::STAGE, "the waves' results fit the stages");
-  __shared__ __attribute__((aligned(16))) char smem[NW * W::STAGE];
+__global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs a) {
+  constexpr int KT = 1 << kPagedFewKeys, NW = 4, OP = D + 4, DEPTH = F8 ? 2 : 1;
+  using W = WaveRows<T, D, KT>;
+  constexpr int SB = W::ST::kBytes > 32 * OP * 4 ? W::ST::kBytes : 32 * OP * 4;  // a wave's LDS: a stage, then its results
+  __shared__ __attribute__((aligned(16))) char smem[NW * SB];
   __shared__ float s_m[NW][32], s_l[NW][32];
   __shared__ int64_t s_scan[NW + 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int T_ = kPagedFewRows >> a.gqa_shift, wg = share_index();
-  const Share share = take_share<256>(a, wg, T_, NW, NW, s_scan);
+  const Share share = take_share<256, kPagedFewWorkgroups, kPagedFewKeys>(a, wg, T_, NW, NW, s_scan);
   const float c = a.scale_log2;
-  char* st = smem + wave * W::STAGE;
-  walk(a, share, wg, T_, [&](const Share& sh, int64_t n, bool whole) {
+  char* st = smem + wave * SB;
+  walk<kPagedFewKeys>(a, share, wg, T_, [&](const Share& sh, int64_t n, bool whole) {
     const SeqShape& q = sh.q;
     const int64_t end = q.end(sh.j), first_pos = q.qb + (int64_t)sh.j * T_;
     W w;
     w.begin(a, q, sh.h, (int64_t)sh.j * kPagedFewRows, lane);
     const int64_t last = sh.kt + n;
     int64_t x = sh.kt + wave;
-    TileRegs<T, D, F8, 1> r;
-    TileKeys cur, nxt;
-    // the rows of tile y, whose pages are in cur, and the pages of the one after it
-    auto ask = [&](int64_t y) {
-      cur.use(a.p);
-      nxt.ask(a.p, sh.s, y + NW, end, lane);
-      cur.template ask_scales<F8>(a.p, sh.h, y, lane);
-      r.load(a.p, sh.h, y, cur.page, 0, lane);
+    // slot i holds a tile's rows and keys; `next` the pages of the one to ask for next
+    TileRegs<T, D, KT, F8, 1> r[DEPTH];
+    TileKeys<KT> key[DEPTH], next;
+    auto ask = [&](int i, int64_t y) __attribute__((always_inline)) {
+      key[i].entry = next.entry;
+      key[i].use(a.p);
+      next.ask(a.p, sh.s, y + NW, end, lane);
+      key[i].template ask_scales<F8>(a.p, sh.h, y, lane);
+      r[i].load(a.p, sh.h, y, key[i].page, 0, lane);
     };
-    if (x < last) {
-      cur.ask(a.p, sh.s, x, end, lane);
-      ask(x);
-    }
+    next.ask(a.p, sh.s, x, end, lane);
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i)
+      if (x + i * NW < last) ask(i, x + i * NW);
     while (x < last) {
-      // positions after the first row lie in this tile, or some are not there
-      const bool masked = x * 64 + 63 > first_pos || cur.ok != ~0ull;
-      const uint64_t bad = r.store(st, cur, masked, 0, lane);
-      const uint64_t ok = cur.ok;
-      __builtin_amdgcn_wave_barrier();
-      if (x + NW < last) {
-        cur = nxt;
-        ask(x + NW);
+#pragma unroll
+      for (int i = 0; i < DEPTH; ++i) {
+        if (x >= last) break;
+        // positions after the first row lie in this tile, or some are not there
+        const uint64_t ok = key[i].ok;
+        const bool masked = x * KT + KT - 1 > first_pos || ok != key[i].kAll;
+        const uint64_t bad = r[i].store(st, key[i], masked, 0, lane);
+        __builtin_amdgcn_wave_barrier();
+        if (x + DEPTH * NW < last) ask(i, x + DEPTH * NW);
+        w.step(st, x, ok, masked, c, lane);
+        if (bad) w.template add_bad<F8>(a.p, sh.s, sh.h, x, bad, lane);
+        __builtin_amdgcn_wave_barrier();
+        x += NW;
       }
-      w.step(st, x, ok, masked, c, lane);
-      if (bad) w.template add_bad<F8>(a.p, sh.s, sh.h, x, bad, lane);
-      __builtin_amdgcn_wave_barrier();
-      x += NW;
     }
     // join the waves: rows as [wave][row][D] through the stages
     const float l = half_sum(w.l);
@@ -588,16 +616,17 @@ __global__ __launch_bounds__(256) void paged_few_kernel(PagedAttnArgs a) {
 // staged in LDS while the one before it is computed.
 template <typename T, int D, bool F8>
 __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs a) {
-  using W = WaveRows<T, D>;
-  constexpr int NW = 8;
-  __shared__ __attribute__((aligned(16))) char smem[2 * W::STAGE];
+  constexpr int KT = 1 << kPagedTileKeys, NW = 8;
+  using W = WaveRows<T, D, KT>;
+  constexpr int SB = W::ST::kBytes;
+  __shared__ __attribute__((aligned(16))) char smem[2 * SB];
   __shared__ int64_t s_scan[NW + 2];
   __shared__ uint64_t s_bad[2][NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int T_ = kPagedTileRows >> a.gqa_shift, wg = share_index();
-  const Share share = take_share<512>(a, wg, T_, 1, 4, s_scan);
+  const Share share = take_share<512, kPagedTileWorkgroups, kPagedTileKeys>(a, wg, T_, 1, 4, s_scan);
   const float c = a.scale_log2;
-  walk(a, share, wg, T_, [&](const Share& sh, int64_t n, bool whole) {
+  walk<kPagedTileKeys>(a, share, wg, T_, [&](const Share& sh, int64_t n, bool whole) {
     const SeqShape& q = sh.q;
     const int64_t end = q.end(sh.j), first_pos = q.qb + (int64_t)sh.j * T_;
     const int64_t nf = (int64_t)q.n << a.gqa_shift, f0 = (int64_t)sh.j * kPagedTileRows + 32 * wave;
@@ -608,8 +637,8 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs a) {
     const int64_t wave_first = q.qb + (f0 >> a.gqa_shift), wave_last = f0 < nf ? q.qb + (f1 >> a.gqa_shift) : -1;
     const int64_t last = sh.kt + n;
     int64_t x = sh.kt;
-    TileRegs<T, D, F8, NW> r;
-    TileKeys cur, nxt;
+    TileRegs<T, D, KT, F8, NW> r;
+    TileKeys<KT> cur, nxt;
     auto ask = [&](int64_t y) {
       cur.use(a.p);
       nxt.ask(a.p, sh.s, y + 1, end, lane);
@@ -618,9 +647,9 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs a) {
     };
     cur.ask(a.p, sh.s, x, end, lane);
     ask(x);
-    auto put = [&](int64_t tile, const TileKeys& k) {
-      const bool masked = tile * 64 + 63 > first_pos || k.ok != ~0ull;
-      const uint64_t bad = r.store(smem + (tile & 1) * W::STAGE, k, masked, wave, lane);
+    auto put = [&](int64_t tile, const TileKeys<KT>& k) {
+      const bool masked = tile * KT + KT - 1 > first_pos || k.ok != k.kAll;
+      const uint64_t bad = r.store(smem + (tile & 1) * SB, k, masked, wave, lane);
       if (masked && lane == 0) s_bad[tile & 1][wave] = bad;
     };
     put(x, cur);
@@ -631,9 +660,9 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs a) {
     }
     __syncthreads();
     for (; x < last; ++x) {
-      const bool staged = x * 64 + 63 > first_pos || ok != ~0ull;
-      if (x * 64 <= wave_last && ok != 0) {  // else no row of the wave attends a key of the tile
-        w.step(smem + (x & 1) * W::STAGE, x, ok, x * 64 + 63 > wave_first || ok != ~0ull, c, lane);
+      const bool staged = x * KT + KT - 1 > first_pos || ok != cur.kAll;
+      if (x * KT <= wave_last && ok != 0) {  // else no row of the wave attends a key of the tile
+        w.step(smem + (x & 1) * SB, x, ok, x * KT + KT - 1 > wave_first || ok != cur.kAll, c, lane);
         if (staged) {
           uint64_t bad = 0;
 #pragma unroll
@@ -696,7 +725,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int m_
   const int4 rec = a.info[wg];
   if (rec.x == 0) return;
   const int T_ = m_rows >> a.gqa_shift;
-  const SeqShape q = shape_of(a, rec.y, T_);
+  const SeqShape q = shape_of<6>(a, rec.y, T_);
   const int64_t nf = (int64_t)q.n << a.gqa_shift, f0 = (int64_t)rec.w * m_rows;
   const int row = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (row >= m_rows || f0 + row >= nf) return;
@@ -729,13 +758,13 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int m_
 
 template <typename T, int D, bool F8>
 static hipError_t attend_dispatch(const PagedAttnArgs& a, bool few, hipStream_t s) {
-  const int m_rows = few ? kPagedFewRows : kPagedTileRows;
-  if (few) hipLaunchKernelGGL((paged_few_kernel<T, D, F8>), dim3(kPagedWorkgroups), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((paged_tile_kernel<T, D, F8>), dim3(kPagedWorkgroups), dim3(512), 0, s, a);
+  const int m_rows = few ? kPagedFewRows : kPagedTileRows, n_wg = paged_workgroups(few);
+  if (few) hipLaunchKernelGGL((paged_few_kernel<T, D, F8>), dim3(n_wg), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_tile_kernel<T, D, F8>), dim3(n_wg), dim3(512), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int rows = a.slot_rows < m_rows ? a.slot_rows : m_rows;
-  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(kPagedWorkgroups, (rows + 7) / 8), dim3(256), 0, s, a, m_rows);
+  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(n_wg, (rows + 7) / 8), dim3(256), 0, s, a, m_rows);
   return hipGetLastError();
 }
 
