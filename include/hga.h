@@ -484,7 +484,7 @@ hga_status_t hga_attend_gathered_bwd(const hga_config_t* cfg, const void* Q, hga
  *               below 2^32 bytes, token strides below 2^27 bytes.
  *   k_scale, v_scale  HGA_CACHE_E4M3: uint8 [n_pages][Hkv][page_size]; else unused.
  *   page_table  int32 [n_seqs][table_cap]. An entry outside [0, n_pages) is an
- *               absent page, as is a position outside the table: rows written
+ *               absent page, as is a position outside the table (or from 2^31 - 128 on): rows written
  *               there are dropped, rows read from there are zeros, and attention
  *               leaves its positions out. Pages may be shared by sequences.
  *   page_size   a power of two in [16, 65536].

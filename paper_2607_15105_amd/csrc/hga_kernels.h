@@ -220,8 +220,8 @@ hipError_t launch_gather_paged(const AttnArgs& a, const PagedArgs& p, int seq, v
 // results that two or more workgroups share. `few`: at most kPagedFewRows
 // folded rows at a time, waves on different keys; else kPagedTileRows folded
 // rows at a time, waves on different rows.
-constexpr int kPagedFewRows = 32;
-constexpr int kPagedTileRows = 256;
+constexpr int kPagedFewRowsLog2 = 5, kPagedFewRows = 1 << kPagedFewRowsLog2;
+constexpr int kPagedTileRowsLog2 = 8, kPagedTileRows = 1 << kPagedTileRowsLog2;
 constexpr int kPagedFewKeys = 5, kPagedTileKeys = 6;  // keys of a unit of work, log2
 constexpr int kPagedFewWorkgroups = 512;   // two per CU
 constexpr int kPagedTileWorkgroups = 256;  // one per CU

@@ -22,40 +22,52 @@ namespace hga {
 
 namespace {
 
+// The kernel's arguments, read where they are used: taken as the parameter they are
+// loaded at the kernel's start and kept in scalars through the loops, of which they
+// take as many as there are (the rest went through vector registers in every
+// tile: 38 moves of 100 instructions that ask for a tile's rows).
+__device__ __forceinline__ const PagedAttnArgs& args_here() {
+  auto p = (const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const PagedAttnArgs*)p;
+}
+
 // ---------------------------------------------------------------- the shares
 
 // The items of a sequence: per kv head nt row tiles of T tokens; row tile j has
-// tiles(j) units.
+// tiles(j) units of 2^KS keys. Positions and tile numbers are 32-bit (kMaxPos).
+template <int KS>
 struct SeqShape {
-  int first, n;      // rows of the call
-  int64_t qb, cap;   // position of the first row; positions that the page table covers
-  int T;             // tokens per row tile
-  int ks;            // keys per unit, log2
-  bool plain;        // all positions inside [0, cap)
+  int first, n;   // rows of the call
+  int qb, cap;    // position of the first row; positions that the page table covers
+  int shift;      // row tiles hold 2^shift tokens
+  bool plain;     // all positions inside [0, cap)
 
-  __device__ inline int nt() const { return (n + T - 1) / T; }
+  __device__ inline int nt() const { return (n + (1 << shift) - 1) >> shift; }
+  // position of row i, clamped to 32 bits
+  __device__ inline int pos(int64_t i) const { return (int)(qb + i < kMaxPos ? qb + i : kMaxPos); }
   // one past the last position that row tile j attends
-  __device__ inline int64_t end(int64_t j) const {
-    const int64_t e = qb + (plain && (j + 1) * T < n ? (j + 1) * T : n);
-    return e < 0 ? 0 : (e > cap ? cap : e);
+  __device__ inline int end(int j) const {
+    const int64_t rows = (int64_t)(j + 1) << shift, e = qb + (plain && rows < n ? rows : n);
+    return e < 0 ? 0 : (e > cap ? cap : (int)e);
   }
   // at least one, so that rows with nothing to attend are written too
-  __device__ inline int64_t tiles(int64_t j) const {
-    const int64_t e = end(j);
-    return e > 0 ? (e + (1 << ks) - 1) >> ks : 1;
+  __device__ inline int tiles(int j) const {
+    const int e = end(j);
+    return e > 0 ? (e + (1 << KS) - 1) >> KS : 1;
   }
-  // units of the row tiles before j <= nt - 1: sum over i < j of ceil((qb + (i+1) T) / 2^ks)
+  // units of the row tiles before j <= nt - 1: sum over i < j of ceil((qb + (i+1) T) / 2^KS)
   __device__ inline int64_t before(int64_t j) const {
     if (j == 0) return 0;
     if (!plain) return j * tiles(0);
-    const int up = (1 << ks) - 1;
-    if (T > up) return j * ((qb + up) >> ks) + (T >> ks) * (j * (j + 1) / 2);
-    const int q = (1 << ks) / T;  // row tiles in which the sum's terms grow by one
-    const int64_t a = j / q;
-    const int b = (int)(j % q);
+    constexpr int up = (1 << KS) - 1;
+    if (shift >= KS) return j * ((qb + up) >> KS) + (((j * (j + 1)) >> 1) << (shift - KS));
+    const int q = 1 << (KS - shift);  // row tiles in which the sum's terms grow by one
+    const int64_t a = j >> (KS - shift);
+    const int b = (int)(j & (q - 1));
     int64_t period = 0, rest = 0;
     for (int i = 1; i <= q; ++i) {
-      const int64_t term = (qb + up + (int64_t)i * T) >> ks;
+      const int64_t term = ((int64_t)qb + up + ((int64_t)i << shift)) >> KS;
       period += term;
       if (i <= b) rest += term;
     }
@@ -65,37 +77,38 @@ struct SeqShape {
 };
 
 template <int KS>
-__device__ inline SeqShape shape_of(const PagedAttnArgs& a, int s, int T) {
-  SeqShape q;
+__device__ inline SeqShape<KS> shape_of(const PagedAttnArgs& a, int s, int shift) {
+  SeqShape<KS> q;
   rows_of(a.p, s, q.first, q.n);
   if (q.n < a.min_rows || q.n > a.max_rows) q.n = 0;
   q.qb = a.p.q_begin[s];
   const int64_t cap = a.p.table_cap << a.p.page_shift;
-  q.cap = cap < ((int64_t)1 << 31) ? cap : (int64_t)1 << 31;
-  q.T = T;
-  q.ks = KS;
-  q.plain = q.qb >= 0 && q.qb + q.n <= q.cap;
+  q.cap = (int)(cap < kMaxPos ? cap : kMaxPos);
+  q.shift = shift;
+  q.plain = q.qb >= 0 && (int64_t)q.qb + q.n <= q.cap;
   return q;
 }
 
-// A workgroup's share [u0, u1) of the units and where it begins.
+// A workgroup's share of the units: `left` of them, and where it begins.
+template <int KS>
 struct Share {
-  int64_t u0, u1, per;
+  int64_t left, per;
   int s, h, j;
-  int64_t kt;   // first unit within the item
-  SeqShape q;   // of sequence s
+  int kt;           // first unit within the item
+  SeqShape<KS> q;   // of sequence s
 };
 
-// NT threads, W workgroups, units of 2^KS keys; `lds` holds NT / 64 + 2 int64.
+// NT threads, W workgroups; `lds` holds NT / 64 + 2 int64. A share is a multiple of `step` units, `least` at least.
 template <int NT, int W, int KS>
-__device__ inline Share take_share(const PagedAttnArgs& a, int wg, int T, int step, int64_t least, int64_t* lds) {
+__device__ inline Share<KS> take_share(int wg, int shift, int step, int least, int64_t* lds) {
   constexpr int NW = NT / 64;
+  const PagedAttnArgs& a = args_here();
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n_seqs = a.p.n_seqs, c = (n_seqs + NT - 1) / NT;
   int64_t sum = 0;
   for (int k = 0; k < c; ++k) {
     const int s = tid * c + k;
-    if (s < n_seqs) sum += a.p.n_kv_heads * shape_of<KS>(a, s, T).units();
+    if (s < n_seqs) sum += a.p.n_kv_heads * shape_of<KS>(a, s, shift).units();
   }
   int64_t inc = sum;
 #pragma unroll
@@ -111,18 +124,16 @@ __device__ inline Share take_share(const PagedAttnArgs& a, int wg, int T, int st
     if (w < wave) base += lds[w];
     total += lds[w];
   }
-  Share sh;
+  Share<KS> sh;
   sh.per = (total + W - 1) / W;
   sh.per = sh.per < least ? least : (sh.per + step - 1) / step * step;
-  sh.u0 = wg * sh.per;
-  sh.u1 = sh.u0 + sh.per;
-  if (sh.u0 > total) sh.u0 = total;
-  if (sh.u1 > total) sh.u1 = total;
-  int64_t off = sh.u0 - (base + inc - sum);
-  if (sh.u0 < sh.u1 && off >= 0 && off < sum) {  // this thread's sequences hold the first unit
+  const int64_t u0 = wg * sh.per;
+  sh.left = u0 >= total ? 0 : total - u0 < sh.per ? total - u0 : sh.per;
+  int64_t off = u0 - (base + inc - sum);
+  if (sh.left > 0 && off >= 0 && off < sum) {  // this thread's sequences hold the first unit
     int s = tid * c;
     for (; s < n_seqs - 1; ++s) {
-      const int64_t m = a.p.n_kv_heads * shape_of<KS>(a, s, T).units();
+      const int64_t m = a.p.n_kv_heads * shape_of<KS>(a, s, shift).units();
       if (off < m) break;
       off -= m;
     }
@@ -130,29 +141,51 @@ __device__ inline Share take_share(const PagedAttnArgs& a, int wg, int T, int st
     lds[NW + 1] = off;
   }
   __syncthreads();
-  sh.s = sh.h = sh.j = 0;
-  sh.kt = 0;
-  if (sh.u0 < sh.u1) {
+  sh.s = sh.h = sh.j = sh.kt = 0;
+  if (sh.left > 0) {
     sh.s = __builtin_amdgcn_readfirstlane((int)lds[NW]);
     off = lds[NW + 1];
-    sh.q = shape_of<KS>(a, sh.s, T);
+    sh.q = shape_of<KS>(a, sh.s, shift);
     const int64_t m = sh.q.units();
-    sh.h = __builtin_amdgcn_readfirstlane((int)(off / m));
+    // kv head and rest: 32-bit division where it will do
+    int h = m < ((int64_t)1 << 31) && off < ((int64_t)1 << 31) ? (int)((uint32_t)off / (uint32_t)m) : (int)(off / m);
+    sh.h = __builtin_amdgcn_readfirstlane(h);
     off -= sh.h * m;
     int lo = 0, hi = sh.q.nt() - 1;  // the last row tile that begins at or before off
     while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
+      const int mid = (int)(((int64_t)lo + hi + 1) >> 1);
       if (sh.q.before(mid) <= off) lo = mid;
       else hi = mid - 1;
     }
     sh.j = __builtin_amdgcn_readfirstlane(lo);
-    sh.kt = off - sh.q.before(sh.j);
+    sh.kt = __builtin_amdgcn_readfirstlane((int)(off - sh.q.before(sh.j)));
   }
   __syncthreads();
   return sh;
 }
 
 // ---------------------------------------------------------------- key tiles
+
+// An item's cached rows: sequence, kv head and last position resolved, in as
+// few scalars as the loops over its tiles need (with the call's arguments in
+// their place 200 of them went through vector registers).
+struct KvItem {
+  const int32_t* table;   // of the sequence
+  const char* k;          // of the kv head
+  const char* v;
+  const uint8_t* k_scale;
+  const uint8_t* v_scale;
+  uint32_t k_page, k_tok, v_page, v_tok, scale_page;  // bytes
+  int n_pages, shift, mask;
+  int end;                // one past the last position that the item attends
+
+  __device__ inline KvItem(const PagedArgs& a, int s, int h, int end_)
+      : table(a.table + (int64_t)s * a.table_cap), k(a.k + h * a.k_head), v(a.v + h * a.v_head),
+        k_scale(a.k_scale + ((int64_t)h << a.page_shift)), v_scale(a.v_scale + ((int64_t)h << a.page_shift)),
+        k_page((uint32_t)a.k_page), k_tok((uint32_t)a.k_tok), v_page((uint32_t)a.v_page), v_tok((uint32_t)a.v_tok),
+        scale_page((uint32_t)a.n_kv_heads << a.page_shift), n_pages(a.n_pages), shift(a.page_shift),
+        mask((1 << a.page_shift) - 1), end(end_) {}
+};
 
 // Pages of a tile's KT positions (32 or 64), a position per lane. `entry` is the table's
 // entry as loaded, or -1; nothing looks at it before use(), so the load can be
@@ -168,20 +201,20 @@ struct TileKeys {
   uint64_t ok;    // positions that are present and before the item's end
   uint32_t ks, vs;  // the rows' scale bytes
 
-  __device__ inline void ask(const PagedArgs& a, int s, int64_t tile, int64_t end, int lane) {
-    const int64_t t = tile * KT + lane, at = t >> a.page_shift;
+  __device__ inline void ask(const KvItem& a, int tile, int lane) {
+    const int t = tile * KT + lane;
     entry = -1;
-    if (lane < KT && t < end && at < a.table_cap) entry = a.table[(int64_t)s * a.table_cap + at];
+    if (lane < KT && t < a.end) entry = a.table[t >> a.shift];
   }
-  __device__ inline void use(const PagedArgs& a) {
+  __device__ inline void use(const KvItem& a) {
     const bool there = (uint32_t)entry < (uint32_t)a.n_pages;
     ok = __ballot(there);
     page = there ? entry : 0;
   }
   template <bool F8>
-  __device__ inline void ask_scales(const PagedArgs& a, int h, int64_t tile, int lane) {
+  __device__ inline void ask_scales(const KvItem& a, int tile, int lane) {
     if constexpr (F8) {
-      const int64_t o = scale_off(a, page, h, (int)((tile * KT + lane) & ((1 << a.page_shift) - 1)));
+      const uint64_t o = (uint64_t)(uint32_t)page * a.scale_page + (uint32_t)((tile * KT + lane) & a.mask);
       ks = a.k_scale[o];
       vs = a.v_scale[o];
     }
@@ -230,8 +263,8 @@ struct Stage {
 };
 
 // One wave's share (of NW waves) of a KT-key tile of K and V, in registers. A
-// load instruction covers R whole rows; pages hold 16 tokens or more, so they lie in
-// one page and the address is a scalar plus a fixed lane offset.
+// load instruction covers R whole rows; pages hold 16 tokens or more, so 16 rows
+// lie in one page and have one scalar address.
 template <typename T, int D, int KT, bool F8, int NW>
 struct TileRegs {
   using TL = Tile<T, D>;
@@ -241,21 +274,22 @@ struct TileRegs {
   static constexpr int R = 64 / PPR;
   static constexpr int NI = KT / R;                   // instructions per tensor
   static constexpr int IPW = 2 * NI / NW;
+  static constexpr int IPB = 16 / R;                  // instructions per 16 rows
   static constexpr int PE = F8 ? 16 : 16 / EB;        // elements of a piece
+  static_assert(IPW % IPB == 0, "a wave loads whole blocks of 16 rows");
   u32x4 w[IPW];
 
-  __device__ inline void load(const PagedArgs& a, int h, int64_t tile, int page, int wave, int lane) {
-    const int mask = (1 << a.page_shift) - 1;
+  __device__ inline void load(const KvItem& a, int tile, int page, int wave, int lane) {
 #pragma unroll
-    for (int i = 0; i < IPW; ++i) {
-      const int j = wave * IPW + i, row = (j % NI) * R;
+    for (int b = 0; b < IPW / IPB; ++b) {
+      const int j = wave * IPW + b * IPB, row = (j % NI) * R;
       const bool v = j >= NI;
-      const int pg = __builtin_amdgcn_readlane(page, row);
-      const int slot = (int)((tile * KT + row) & mask);
-      const int64_t tok = v ? a.v_tok : a.k_tok;
-      const char* base = v ? a.v + page_off(pg, slot, a.v_page, tok) + h * a.v_head
-                           : a.k + page_off(pg, slot, a.k_page, tok) + h * a.k_head;
-      w[i] = *reinterpret_cast<const u32x4*>(base + (uint32_t)((lane / PPR) * (uint32_t)tok + (lane % PPR) * 16));
+      const uint32_t pg = (uint32_t)__builtin_amdgcn_readlane(page, row), slot = (uint32_t)((tile * KT + row) & a.mask);
+      const uint32_t tok = v ? a.v_tok : a.k_tok;
+      const char* base = (v ? a.v : a.k) + ((uint64_t)pg * (v ? a.v_page : a.k_page) + (uint64_t)slot * tok);
+#pragma unroll
+      for (int i = 0; i < IPB; ++i)
+        w[b * IPB + i] = *reinterpret_cast<const u32x4*>(base + (uint32_t)((lane / PPR + i * R) * tok + (lane % PPR) * 16));
     }
   }
 
@@ -333,14 +367,15 @@ struct WaveRows {
   Frag qf[NKS];
   f32x16 oacc[NDT];
   float m, l;
-  int64_t pos;  // of the lane's row; -1 for a row past the item's rows
+  int pos;  // of the lane's row; -1 for a row past the item's rows
 
   // Rows of the item from folded row f0 on (of nf rows of the sequence).
-  __device__ inline void begin(const PagedAttnArgs& a, const SeqShape& q, int h, int64_t f0, int lane) {
+  template <typename Q>
+  __device__ inline void begin(const PagedAttnArgs& a, const Q& q, int h, int64_t f0, int lane) {
     const int hh = lane >> 5;
     const int64_t nf = (int64_t)q.n << a.gqa_shift;
     int64_t f = f0 + (lane & 31);
-    pos = f < nf ? q.qb + (f >> a.gqa_shift) : -1;
+    pos = f < nf ? q.pos(f >> a.gqa_shift) : -1;
     if (f >= nf) f = nf - 1;
     const int64_t row = q.first + (f >> a.gqa_shift);
     const int hq = (h << a.gqa_shift) + (int)(f & ((1 << a.gqa_shift) - 1));
@@ -354,7 +389,7 @@ struct WaveRows {
   }
 
   // One tile from its LDS stage. masked: keys that are not ok or after the row do not count.
-  __device__ __forceinline__ void step(const char* st, int64_t tile, uint64_t ok, bool masked, float c, int lane) {
+  __device__ __forceinline__ void step(const char* st, int tile, uint64_t ok, bool masked, float c, int lane) {
     const int hh = lane >> 5, l32 = lane & 31;
     const float lazy = 8.0f / c;
     f32x16 s[NH];
@@ -368,7 +403,7 @@ struct WaveRows {
         s[t] = EL::mma(kf, qf[ks], s[t]);
       }
     if (masked) {
-      const int64_t rel = pos - tile * KT;  // keys 0 .. rel are at or before the row
+      const int rel = pos < 0 ? -1 : pos - tile * KT;  // keys 0 .. rel are at or before the row
       const uint64_t see = (ok & (rel < 0 ? 0 : rel >= 63 ? ~0ull : (2ull << rel) - 1)) >> (4 * hh);
 #pragma unroll
       for (int t = 0; t < NH; ++t)
@@ -421,16 +456,14 @@ struct WaveRows {
   // would bring it to rows that do not attend its key): added here to the
   // rows that do.
   template <bool F8>
-  __device__ inline void add_bad(const PagedArgs& a, int s, int h, int64_t tile, uint64_t bad, int lane) {
+  __device__ inline void add_bad(const KvItem& a, int tile, uint64_t bad, int lane) {
     const int hh = lane >> 5;
     while (bad) {
       const int kk = __builtin_ctzll(bad);
       bad &= bad - 1;
-      const int64_t t = tile * KT + kk;
-      const int page = page_of(a, s, t);
-      if (page < 0 || pos < t) continue;
-      const int slot = (int)(t & ((1 << a.page_shift) - 1));
-      const char* row = a.v + page_off(page, slot, a.v_page, a.v_tok) + h * a.v_head;
+      const int t = tile * KT + kk;
+      if (pos < t) continue;
+      const char* row = a.v + page_off(a.table[t >> a.shift], t & a.mask, a.v_page, a.v_tok);  // a row of the tile: present
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
@@ -441,6 +474,7 @@ struct WaveRows {
           else if constexpr (EB == 2) x = bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(row + 2 * d));
           else x = *reinterpret_cast<const float*>(row + 4 * d);
           if (!(fabsf(x) < __builtin_inff())) oacc[dt][v] += x;
+          __builtin_amdgcn_sched_barrier(0);  // one at a time: all at once, the comparisons take the loops' scalars
         }
     }
   }
@@ -470,32 +504,29 @@ __device__ inline float lse_of(float m, float l, float c) {
 // on one XCD (workgroups are dealt round-robin to the eight), whose L2 then holds what they share.
 __device__ inline int share_index() { return (blockIdx.x & 7) * (gridDim.x / 8) + (blockIdx.x >> 3); }
 
-// Follows a share item by item: f(s, q, h, j, first tile, tiles, whole) and the record of the one left unfinished.
+// Follows a share item by item: f(share at the item, tiles of it, whether that is all of it), and the record of the one left unfinished.
 template <int KS, typename F>
-__device__ inline void walk(const PagedAttnArgs& a, Share sh, int wg, int T, F&& f) {
-  int64_t u = sh.u0;
-  if (threadIdx.x == 0) a.info[wg] = make_int4(0, 0, 0, 0);
-  while (u < sh.u1) {
-    const int64_t len = sh.q.tiles(sh.j), left = len - sh.kt;
-    const int64_t n = left < sh.u1 - u ? left : sh.u1 - u;
-    const bool whole = n == len;
+__device__ inline void walk(Share<KS> sh, int wg, int shift, F&& f) {
+  if (threadIdx.x == 0) args_here().info[wg] = make_int4(0, 0, 0, 0);
+  while (sh.left > 0) {
+    const int len = sh.q.tiles(sh.j), rest = len - sh.kt;
+    const int n = rest < sh.left ? rest : (int)sh.left;
     if (sh.kt == 0 && n < len) {  // goes on in the next shares: this one joins it
       const int64_t more = len - n;
-      if (threadIdx.x == 0) a.info[wg] = make_int4((int)(1 + (more + sh.per - 1) / sh.per), sh.s, sh.h, sh.j);
+      if (threadIdx.x == 0) args_here().info[wg] = make_int4((int)(1 + (more + sh.per - 1) / sh.per), sh.s, sh.h, sh.j);
     }
-    f(sh, n, whole);
-    u += n;
+    f(sh, n, n == len);
+    sh.left -= n;
     sh.kt = 0;
-    if (u < sh.u1) {
-      if (++sh.j == sh.q.nt()) {
-        sh.j = 0;
-        if (++sh.h == a.p.n_kv_heads) {
-          sh.h = 0;
-          do {
-            if (++sh.s >= a.p.n_seqs) return;  // not reached: units remain, so a sequence with rows does
-            sh.q = shape_of<KS>(a, sh.s, T);
-          } while (sh.q.n == 0);
-        }
+    if (sh.left > 0 && ++sh.j == sh.q.nt()) {
+      const PagedAttnArgs& a = args_here();
+      sh.j = 0;
+      if (++sh.h == a.p.n_kv_heads) {
+        sh.h = 0;
+        do {
+          if (++sh.s >= a.p.n_seqs) return;  // not reached: units remain, so a sequence with rows does
+          sh.q = shape_of<KS>(a, sh.s, shift);
+        } while (sh.q.n == 0);
       }
     }
   }
@@ -512,7 +543,7 @@ __device__ inline void walk(const PagedAttnArgs& a, Share sh, int wg, int T, F&&
 // are asked for two tiles ahead, which keeps as many bytes under way as one of
 // bf16 rows does (16 KB a wave, 128 KB a CU).
 template <typename T, int D, bool F8>
-__global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs) {
   constexpr int KT = 1 << kPagedFewKeys, NW = 4, OP = D + 4, DEPTH = F8 ? 2 : 1;
   using W = WaveRows<T, D, KT>;
   constexpr int SB = W::ST::kBytes > 32 * OP * 4 ? W::ST::kBytes : 32 * OP * 4;  // a wave's LDS: a stage, then its results
@@ -520,28 +551,30 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs a) {
   __shared__ float s_m[NW][32], s_l[NW][32];
   __shared__ int64_t s_scan[NW + 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int T_ = kPagedFewRows >> a.gqa_shift, wg = share_index();
-  const Share share = take_share<256, kPagedFewWorkgroups, kPagedFewKeys>(a, wg, T_, NW, NW, s_scan);
-  const float c = a.scale_log2;
+  const int shift = kPagedFewRowsLog2 - args_here().gqa_shift, wg = share_index();
+  const Share<kPagedFewKeys> share = take_share<256, kPagedFewWorkgroups, kPagedFewKeys>(wg, shift, NW, NW, s_scan);
+  const float c = args_here().scale_log2;
   char* st = smem + wave * SB;
-  walk<kPagedFewKeys>(a, share, wg, T_, [&](const Share& sh, int64_t n, bool whole) {
-    const SeqShape& q = sh.q;
-    const int64_t end = q.end(sh.j), first_pos = q.qb + (int64_t)sh.j * T_;
+  walk(share, wg, shift, [&](const Share<kPagedFewKeys>& sh, int n, bool whole) {
+    const SeqShape<kPagedFewKeys>& q = sh.q;
+    const PagedAttnArgs& a0 = args_here();
+    const int first_pos = q.pos((int64_t)sh.j << shift);
+    const KvItem kv(a0.p, sh.s, sh.h, q.end(sh.j));
     W w;
-    w.begin(a, q, sh.h, (int64_t)sh.j * kPagedFewRows, lane);
-    const int64_t last = sh.kt + n;
-    int64_t x = sh.kt + wave;
+    w.begin(a0, q, sh.h, (int64_t)sh.j * kPagedFewRows, lane);
+    const int last = sh.kt + n;
+    int x = sh.kt + wave;
     // slot i holds a tile's rows and keys; `next` the pages of the one to ask for next
     TileRegs<T, D, KT, F8, 1> r[DEPTH];
     TileKeys<KT> key[DEPTH], next;
-    auto ask = [&](int i, int64_t y) __attribute__((always_inline)) {
+    auto ask = [&](int i, int y) __attribute__((always_inline)) {
       key[i].entry = next.entry;
-      key[i].use(a.p);
-      next.ask(a.p, sh.s, y + NW, end, lane);
-      key[i].template ask_scales<F8>(a.p, sh.h, y, lane);
-      r[i].load(a.p, sh.h, y, key[i].page, 0, lane);
+      key[i].use(kv);
+      next.ask(kv, y + NW, lane);
+      key[i].template ask_scales<F8>(kv, y, lane);
+      r[i].load(kv, y, key[i].page, 0, lane);
     };
-    next.ask(a.p, sh.s, x, end, lane);
+    next.ask(kv, x, lane);
 #pragma unroll
     for (int i = 0; i < DEPTH; ++i)
       if (x + i * NW < last) ask(i, x + i * NW);
@@ -556,12 +589,13 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs a) {
         __builtin_amdgcn_wave_barrier();
         if (x + DEPTH * NW < last) ask(i, x + DEPTH * NW);
         w.step(st, x, ok, masked, c, lane);
-        if (bad) w.template add_bad<F8>(a.p, sh.s, sh.h, x, bad, lane);
+        if (bad) w.template add_bad<F8>(kv, x, bad, lane);
         __builtin_amdgcn_wave_barrier();
         x += NW;
       }
     }
     // join the waves: rows as [wave][row][D] through the stages
+    const PagedAttnArgs& a = args_here();
     const float l = half_sum(w.l);
     __syncthreads();
     float* so = reinterpret_cast<float*>(smem);
@@ -615,7 +649,7 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs a) {
 // 256 folded rows per item, 32 per wave; the waves share each tile, which is
 // staged in LDS while the one before it is computed.
 template <typename T, int D, bool F8>
-__global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
   constexpr int KT = 1 << kPagedTileKeys, NW = 8;
   using W = WaveRows<T, D, KT>;
   constexpr int SB = W::ST::kBytes;
@@ -623,31 +657,33 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs a) {
   __shared__ int64_t s_scan[NW + 2];
   __shared__ uint64_t s_bad[2][NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int T_ = kPagedTileRows >> a.gqa_shift, wg = share_index();
-  const Share share = take_share<512, kPagedTileWorkgroups, kPagedTileKeys>(a, wg, T_, 1, 4, s_scan);
-  const float c = a.scale_log2;
-  walk<kPagedTileKeys>(a, share, wg, T_, [&](const Share& sh, int64_t n, bool whole) {
-    const SeqShape& q = sh.q;
-    const int64_t end = q.end(sh.j), first_pos = q.qb + (int64_t)sh.j * T_;
-    const int64_t nf = (int64_t)q.n << a.gqa_shift, f0 = (int64_t)sh.j * kPagedTileRows + 32 * wave;
+  const int shift = kPagedTileRowsLog2 - args_here().gqa_shift, wg = share_index();
+  const Share<kPagedTileKeys> share = take_share<512, kPagedTileWorkgroups, kPagedTileKeys>(wg, shift, 1, 4, s_scan);
+  const float c = args_here().scale_log2;
+  walk(share, wg, shift, [&](const Share<kPagedTileKeys>& sh, int n, bool whole) {
+    const SeqShape<kPagedTileKeys>& q = sh.q;
+    const PagedAttnArgs& a0 = args_here();
+    const int first_pos = q.pos((int64_t)sh.j << shift);
+    const KvItem kv(a0.p, sh.s, sh.h, q.end(sh.j));
+    const int64_t nf = (int64_t)q.n << a0.gqa_shift, f0 = (int64_t)sh.j * kPagedTileRows + 32 * wave;
     W w;
-    w.begin(a, q, sh.h, f0, lane);
+    w.begin(a0, q, sh.h, f0, lane);
     // the wave's rows lie at positions wave_first .. wave_last; none if f0 >= nf
     const int64_t f1 = f0 + 31 < nf ? f0 + 31 : nf - 1;
-    const int64_t wave_first = q.qb + (f0 >> a.gqa_shift), wave_last = f0 < nf ? q.qb + (f1 >> a.gqa_shift) : -1;
-    const int64_t last = sh.kt + n;
-    int64_t x = sh.kt;
+    const int wave_first = q.pos(f0 >> a0.gqa_shift), wave_last = f0 < nf ? q.pos(f1 >> a0.gqa_shift) : -1;
+    const int last = sh.kt + n;
+    int x = sh.kt;
     TileRegs<T, D, KT, F8, NW> r;
     TileKeys<KT> cur, nxt;
-    auto ask = [&](int64_t y) {
-      cur.use(a.p);
-      nxt.ask(a.p, sh.s, y + 1, end, lane);
-      cur.template ask_scales<F8>(a.p, sh.h, y, lane);
-      r.load(a.p, sh.h, y, cur.page, wave, lane);
+    auto ask = [&](int y) {
+      cur.use(kv);
+      nxt.ask(kv, y + 1, lane);
+      cur.template ask_scales<F8>(kv, y, lane);
+      r.load(kv, y, cur.page, wave, lane);
     };
-    cur.ask(a.p, sh.s, x, end, lane);
+    cur.ask(kv, x, lane);
     ask(x);
-    auto put = [&](int64_t tile, const TileKeys<KT>& k) {
+    auto put = [&](int tile, const TileKeys<KT>& k) {
       const bool masked = tile * KT + KT - 1 > first_pos || k.ok != k.kAll;
       const uint64_t bad = r.store(smem + (tile & 1) * SB, k, masked, wave, lane);
       if (masked && lane == 0) s_bad[tile & 1][wave] = bad;
@@ -667,7 +703,7 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs a) {
           uint64_t bad = 0;
 #pragma unroll
           for (int k = 0; k < NW; ++k) bad |= s_bad[x & 1][k];
-          if (bad) w.template add_bad<F8>(a.p, sh.s, sh.h, x, bad, lane);
+          if (bad) w.template add_bad<F8>(kv, x, bad, lane);
         }
       }
       if (x + 1 < last) {
@@ -680,6 +716,7 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs a) {
       }
       __syncthreads();
     }
+    const PagedAttnArgs& a = args_here();
     const float l = half_sum(w.l);
     const int hh = lane >> 5, l32 = lane & 31;
     const int64_t f = f0 + l32;
@@ -717,41 +754,65 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs a) {
 // ---------------------------------------------------------------- the joining
 
 // An item that shares w, w + 1, ... cut: its parts in the order of the keys. A
-// workgroup joins eight rows, 32 lanes each.
+// workgroup joins eight rows, 32 lanes each: the lanes read 32 parts' maxima and
+// sums at once and hand the weights round, and the parts' rows are read eight
+// at a time. What bounds it is that chain of four round trips.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int m_rows) {
   constexpr int EB = Elem<T>::kBytes, V = D / 32;
+  typedef float fV __attribute__((ext_vector_type(V)));
   const int wg = blockIdx.x;
   const int4 rec = a.info[wg];
   if (rec.x == 0) return;
-  const int T_ = m_rows >> a.gqa_shift;
-  const SeqShape q = shape_of<6>(a, rec.y, T_);
+  const SeqShape<6> q = shape_of<6>(a, rec.y, 0);
   const int64_t nf = (int64_t)q.n << a.gqa_shift, f0 = (int64_t)rec.w * m_rows;
   const int row = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (row >= m_rows || f0 + row >= nf) return;
   const float c = a.scale_log2;
   // part k is the share wg + k's: the first one its last item, the others their first
   auto at = [&](int k) { return ((int64_t)(wg + k) * 2 + (k == 0 ? 1 : 0)) * a.slot_rows + row; };
-  float M = -__builtin_inff();
-  for (int k = lane; k < rec.x; k += 32) M = fmaxf(M, a.part_ml[at(k) * 2]);
+  float M = -__builtin_inff(), L = 0.0f;
+  fV o = fV{};
+  for (int k0 = 0; k0 < rec.x; k0 += 32) {
+    const int n = rec.x - k0 < 32 ? rec.x - k0 : 32;
+    float m = -__builtin_inff(), l = 0.0f;
+    if (lane < n) {
+      m = a.part_ml[at(k0 + lane) * 2];
+      l = a.part_ml[at(k0 + lane) * 2 + 1];
+    }
+    float mx = m;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
-  float L = 0.0f, o[V] = {};
-  for (int k = 0; k < rec.x; ++k) {
-    const float m = a.part_ml[at(k) * 2], l = a.part_ml[at(k) * 2 + 1];
+    for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 32));
+    if (mx > M) {
+      const float f = __builtin_amdgcn_exp2f((M - mx) * c);
+      L *= f;
+      o *= f;
+      M = mx;
+    }
     const float f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - M) * c);
-    L += l * f;
-    const float* src = a.part + at(k) * D + lane * V;
+    l *= f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) o[v] += src[v] * f;
+    for (int d = 16; d > 0; d >>= 1) l += __shfl_xor(l, d, 32);
+    L += l;
+    for (int k = 0; k < n; k += 8) {
+      fV x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        x[i] = *reinterpret_cast<const fV*>(a.part + at(k0 + (k + i < n ? k + i : n - 1)) * D + lane * V);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float w = __shfl(f, k + i < n ? k + i : 0, 32);
+        if (k + i < n) o += x[i] * w;
+      }
+    }
   }
-  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+  o *= L == 0.0f ? 0.0f : 1.0f / L;
   float* lse;
   char* dst = out_row(a, q.first, rec.z, f0 + row, lse) + lane * V * EB;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    if constexpr (EB == 2) reinterpret_cast<uint16_t*>(dst)[v] = (uint16_t)float_to_bf16_bits(o[v] * inv);
-    else reinterpret_cast<float*>(dst)[v] = o[v] * inv;
+    if constexpr (EB == 2) reinterpret_cast<uint16_t*>(dst)[v] = (uint16_t)float_to_bf16_bits(o[v]);
+    else reinterpret_cast<float*>(dst)[v] = o[v];
   }
   if (lane == 0) *lse = lse_of(M, L, c);
 }

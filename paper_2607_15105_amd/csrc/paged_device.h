@@ -62,10 +62,14 @@ template <> struct Codes<float> {
   }
 };
 
+// Positions from here on count as outside the page table, so that a position, one
+// past it and the tile that holds it fit 32 bits.
+constexpr int kMaxPos = 0x7fffff80;
+
 // Page of position t (any value) of sequence s, -1 if it is absent: outside the
 // table, or an entry outside [0, n_pages).
 __device__ inline int page_of(const PagedArgs& a, int s, int64_t t) {
-  if (t < 0 || (t >> a.page_shift) >= a.table_cap) return -1;
+  if (t < 0 || t >= kMaxPos || (t >> a.page_shift) >= a.table_cap) return -1;
   const int p = a.table[(int64_t)s * a.table_cap + (t >> a.page_shift)];
   return (uint32_t)p < (uint32_t)a.n_pages ? p : -1;
 }
