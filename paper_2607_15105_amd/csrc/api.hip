@@ -902,24 +902,40 @@ hga_status_t hga_gather_paged(const hga_config_t* cfg, const hga_paged_cache_t* 
   return HGA_OK;
 }
 
+using hga::PagedForm;
 // Folded rows (row, query head of a kv head) of a partial result's slot, and a form's scratch.
-static int64_t slot_rows(const hga_config_t* c, int64_t n_rows, bool few) {
-  const int64_t f = n_rows * (c->n_q_heads / c->n_kv_heads), m = few ? hga::kPagedFewRows : hga::kPagedTileRows;
-  return f < m ? f : m;
+static int slot_rows(const hga_config_t* c, int64_t n_rows, PagedForm form) {
+  const int64_t f = n_rows * (c->n_q_heads / c->n_kv_heads);
+  return f < hga::paged_rows(form) ? (int)f : hga::paged_rows(form);
 }
-static size_t paged_ws(const hga_config_t* c, int64_t n_rows, bool few) {
-  const size_t rows = 2 * (size_t)hga::paged_workgroups(few) * slot_rows(c, n_rows, few);
-  return hga::paged_workgroups(few) * sizeof(int4) + rows * (c->head_dim + 2) * sizeof(float);
+static size_t paged_ws(const hga_config_t* c, int64_t n_rows, PagedForm form) {
+  const size_t rows = 2 * (size_t)hga::paged_workgroups(form) * slot_rows(c, n_rows, form);
+  return hga::paged_workgroups(form) * sizeof(int4) + rows * (c->head_dim + 2) * sizeof(float);
 }
-// Whether no sequence is expected to have more rows than the form for few takes at a time.
-static bool only_few(const hga_config_t* c, int64_t max_rows) {
-  return max_rows <= hga::kPagedFewRows / (c->n_q_heads / c->n_kv_heads);
+// The forms a call runs, one after the other: of few rows only where no sequence is
+// expected to have more than that form takes at a time; else the form of many
+// rows, and for the sequences of few rows beside them (generation beside a
+// prompt's chunk) that of 16. A form of its own takes whatever there is.
+static int paged_forms(const hga_config_t* c, int64_t n_seqs, int64_t max_rows, PagedForm (&forms)[2]) {
+  const int64_t folded = max_rows < 64 ? max_rows * (c->n_q_heads / c->n_kv_heads) : 64;
+  if (folded <= 32) {
+    forms[0] = folded <= 16 ? PagedForm::kFew16 : PagedForm::kFew32;
+    return 1;
+  }
+  forms[0] = PagedForm::kTile;
+  forms[1] = PagedForm::kFew16;
+  return n_seqs > 1 ? 2 : 1;
 }
 
 size_t hga_paged_workspace_size(const hga_config_t* cfg, int64_t n_rows, int64_t max_rows) {
   if (check_cfg(cfg) != HGA_OK || n_rows < 1 || n_rows >= kMaxTokens || max_rows < 1) return 0;
-  const size_t few = paged_ws(cfg, n_rows, true), tile = paged_ws(cfg, n_rows, false);
-  return only_few(cfg, max_rows) || few > tile ? few : tile;
+  PagedForm forms[2];
+  size_t most = 0;
+  for (int i = 0, n = paged_forms(cfg, 2, max_rows, forms); i < n; ++i) {
+    const size_t need = paged_ws(cfg, n_rows, forms[i]);
+    if (need > most) most = need;
+  }
+  return most;
 }
 
 hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache_t* cache, const void* Q,
@@ -944,20 +960,17 @@ hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache
   a.scale_log2 = eff_scale(cfg) * 1.4426950408889634f;
   a.info = static_cast<int4*>(workspace);
   const bool e4m3 = cache->format == HGA_CACHE_E4M3, bf16 = cfg->dtype == HGA_BF16;
-  // Each form takes the sequences whose rows suit it; the two share the
-  // workspace, one after the other on the stream. A single sequence, and a call
-  // of few rows, needs one form only, which then takes whatever there is.
-  const int few_rows = hga::kPagedFewRows / G;
-  const bool few = only_few(cfg, max_rows), both = !few && cache->n_seqs > 1;
-  for (int form = 0; form < 2; ++form) {
-    const bool is_few = form == 0;
-    if (!both && is_few != few) continue;
-    a.min_rows = both && !is_few ? few_rows + 1 : 1;
-    a.max_rows = both && is_few ? few_rows : 0x7fffffff;
-    a.slot_rows = (int)slot_rows(cfg, n_rows, is_few);
-    a.part = reinterpret_cast<float*>(a.info + hga::paged_workgroups(is_few));
-    a.part_ml = a.part + 2 * (int64_t)hga::paged_workgroups(is_few) * a.slot_rows * cfg->head_dim;
-    if (hga::launch_attend_paged(a, is_few, e4m3, bf16, cfg->head_dim, (hipStream_t)stream) != hipSuccess)
+  PagedForm forms[2];
+  const int n_forms = paged_forms(cfg, cache->n_seqs, max_rows, forms);
+  for (int i = 0; i < n_forms; ++i) {  // they share the workspace
+    const PagedForm form = forms[i];
+    const int few_rows = 16 / G;
+    a.min_rows = n_forms == 2 && form == PagedForm::kTile ? few_rows + 1 : 1;
+    a.max_rows = n_forms == 2 && form != PagedForm::kTile ? few_rows : 0x7fffffff;
+    a.slot_rows = slot_rows(cfg, n_rows, form);
+    a.part = reinterpret_cast<float*>(a.info + hga::paged_workgroups(form));
+    a.part_ml = a.part + 2 * (int64_t)hga::paged_workgroups(form) * a.slot_rows * cfg->head_dim;
+    if (hga::launch_attend_paged(a, form, e4m3, bf16, cfg->head_dim, (hipStream_t)stream) != hipSuccess)
       return HGA_ERR_HIP;
   }
   return HGA_OK;

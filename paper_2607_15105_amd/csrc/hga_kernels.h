@@ -216,16 +216,18 @@ hipError_t launch_cache_read(const PagedArgs& a, const DenseRows& d, bool e4m3, 
 // routing, as launch_gather's; p.seq_rows / q_begin unused).
 hipError_t launch_gather_paged(const AttnArgs& a, const PagedArgs& p, int seq, void* kc, void* vc, bool e4m3, bool bf16,
                                int head_dim, hipStream_t s);
-// Attention over the cache in two forms, each followed by the joining of the
-// results that two or more workgroups share. `few`: at most kPagedFewRows
-// folded rows at a time, waves on different keys; else kPagedTileRows folded
-// rows at a time, waves on different rows.
-constexpr int kPagedFewRowsLog2 = 5, kPagedFewRows = 1 << kPagedFewRowsLog2;
+// Attention over the cache, followed by the joining of the results that two or
+// more workgroups share, in three forms: 16 or 32 folded rows at a time, waves on
+// different keys, or 256, waves on different rows.
+enum class PagedForm { kFew16, kFew32, kTile };
+constexpr int paged_rows(PagedForm f) { return f == PagedForm::kFew16 ? 16 : f == PagedForm::kFew32 ? 32 : 256; }
 constexpr int kPagedTileRowsLog2 = 8, kPagedTileRows = 1 << kPagedTileRowsLog2;
-constexpr int kPagedFewKeys = 5, kPagedTileKeys = 6;  // keys of a unit of work, log2
+// keys of a unit of work, log2
+constexpr int few_unit_keys(bool e4m3) { return e4m3 ? 6 : 5; }
+constexpr int kPagedTileKeys = 6;
 constexpr int kPagedFewWorkgroups = 512;   // two per CU
 constexpr int kPagedTileWorkgroups = 256;  // one per CU
-inline int paged_workgroups(bool few) { return few ? kPagedFewWorkgroups : kPagedTileWorkgroups; }
-hipError_t launch_attend_paged(const PagedAttnArgs& a, bool few, bool e4m3, bool bf16, int head_dim, hipStream_t s);
+constexpr int paged_workgroups(PagedForm f) { return f == PagedForm::kTile ? kPagedTileWorkgroups : kPagedFewWorkgroups; }
+hipError_t launch_attend_paged(const PagedAttnArgs& a, PagedForm form, bool e4m3, bool bf16, int head_dim, hipStream_t s);
 
 }  // namespace hga

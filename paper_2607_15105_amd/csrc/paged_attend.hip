@@ -185,41 +185,60 @@ struct KvItem {
         k_page((uint32_t)a.k_page), k_tok((uint32_t)a.k_tok), v_page((uint32_t)a.v_page), v_tok((uint32_t)a.v_tok),
         scale_page((uint32_t)a.n_kv_heads << a.page_shift), n_pages(a.n_pages), shift(a.page_shift),
         mask((1 << a.page_shift) - 1), end(end_) {}
+
+  // V's row of position t, which is present.
+  __device__ inline const char* v_row(int t) const { return v + page_off(table[t >> shift], t & mask, v_page, v_tok); }
 };
 
-// Pages of a tile's KT positions (32 or 64), a position per lane. `entry` is the table's
-// entry as loaded, or -1; nothing looks at it before use(), so the load can be
-// under way beside the tile before it. (Loads return in order: a wait for the
-// entry right after it was asked for is a wait for every row asked for before
-// it. With that, 64 ragged contexts took 343 us, 8-bit rows; a 2,048-token chunk at the
-// end of 32K 1,383 us.)
-template <int KT>
-struct TileKeys {
-  static constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << KT) - 1;
-  int entry;
-  int page;       // 0 where there is none
-  uint64_t ok;    // positions that are present and before the item's end
-  uint32_t ks, vs;  // the rows' scale bytes
+// Where 64 tiles of an item lie: lane i has the pages of tile x0 + i * STRIDE, a tile
+// of KT positions, for the BLOCKS blocks of 16 rows from block b0 on; page 0
+// where there is none. Asked for 64 tiles at a time, so that a tile costs a lane
+// read and a bit test. (Asked for tile by tile, beside the tile before: 64
+// ragged contexts in 8 bits 187 us, a 2,048-token chunk at the end of 32K 1,097 us;
+// waited for where it was asked for: 343 and 1,383 us.)
+template <int KT, int STRIDE, int BLOCKS>
+struct TileMap {
+  int page[BLOCKS];
+  uint64_t full;   // bit i: every position of tile x0 + i * STRIDE is present and before the item's end
 
-  __device__ inline void ask(const KvItem& a, int tile, int lane) {
-    const int t = tile * KT + lane;
-    entry = -1;
-    if (lane < KT && t < a.end) entry = a.table[t >> a.shift];
-  }
-  __device__ inline void use(const KvItem& a) {
-    const bool there = (uint32_t)entry < (uint32_t)a.n_pages;
-    ok = __ballot(there);
-    page = there ? entry : 0;
-  }
-  template <bool F8>
-  __device__ inline void ask_scales(const KvItem& a, int tile, int lane) {
-    if constexpr (F8) {
-      const uint64_t o = (uint64_t)(uint32_t)page * a.scale_page + (uint32_t)((tile * KT + lane) & a.mask);
-      ks = a.k_scale[o];
-      vs = a.v_scale[o];
+  __device__ inline void fill(const KvItem& a, int x0, int b0, int lane) {
+    const int64_t t = ((int64_t)x0 + (int64_t)STRIDE * lane) * KT;
+    bool all = t + KT <= a.end;
+    int e[KT / 16];
+#pragma unroll
+    for (int b = 0; b < KT / 16; ++b) {
+      e[b] = -1;
+      if (t + 16 * b < a.end) e[b] = a.table[(int)(t + 16 * b) >> a.shift];
     }
+#pragma unroll
+    for (int b = 0; b < KT / 16; ++b) {
+      if ((uint32_t)e[b] >= (uint32_t)a.n_pages) {
+        all = false;
+        e[b] = 0;
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) page[b] = e[b];
+    if constexpr (BLOCKS == 1) {
+#pragma unroll
+      for (int b = 1; b < KT / 16; ++b)
+        if (b == b0) page[0] = e[b];
+    }
+    full = __ballot(all);
   }
 };
+
+template <int KT>
+__device__ inline constexpr uint64_t all_keys() { return KT == 64 ? ~0ull : (1ull << (KT & 63)) - 1; }
+
+// The positions of a tile that are present and before the item's end.
+template <int KT>
+__device__ inline uint64_t present(const KvItem& a, int tile, int lane) {
+  const int t = tile * KT + lane;
+  int e = -1;
+  if (lane < KT && t < a.end) e = a.table[t >> a.shift];
+  return __ballot((uint32_t)e < (uint32_t)a.n_pages);
+}
 
 template <typename T>
 __device__ inline bool finite16(const uint4& w) {
@@ -252,23 +271,51 @@ __device__ inline uint4 only_finite(const uint4& w) {
 
 // One LDS stage of a KT-key tile: K rows, then V (rows, or transposed for
 // float32, which has no transposing LDS load).
-template <typename T, int D, int KT>
+template <typename T, int D, int KT_>
 struct Stage {
   using TL = Tile<T, D>;
+  static constexpr int KT = KT_;
   static constexpr bool TR = Elem<T>::kBytes == 2;
   static constexpr int kV = KT * TL::kRowPitch;  // offset of V
   static constexpr int kBytes = kV + (TR ? KT * TL::kRowPitch : D * (KT + 1) * 4);
   // element (d, kpos) of the transposed V
   __device__ static inline int t_off(int d, int kpos) { return kV + (d * (KT + 1) + kpos) * 4; }
+  // 16 bytes of row `row` from element e on
+  __device__ static inline void put(char* st, bool v, int row, int e, const uint4& w) {
+    if (TR || !v) {
+      *reinterpret_cast<uint4*>(st + (v ? kV : 0) + TL::row_off(row, e)) = w;
+    } else {
+      const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+      const int kp = kpos_of<Elem<T>::E>(row);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) *reinterpret_cast<uint32_t*>(st + t_off(e + y, kp)) = x[y];
+    }
+  }
+};
+
+// The same for the 16-row products: both tensors in rows. An operand load of K
+// takes one 16-byte piece of 16 rows, whose rows 16 bytes over a multiple of 256 (or
+// 128) put them on all banks. bf16 V is read transposed, 32 lanes taking 32 bytes
+// of eight consecutive rows: those 32 bytes over do the same. float32 V is
+// read as it lies, 64 bytes of rows four apart, for which 16 bytes over are right.
+template <typename T, int D>
+struct FewStage {
+  static constexpr int KT = 32, EB = Elem<T>::kBytes;
+  static constexpr int kPitch = D * EB + 16, kVPitch = D * EB + (EB == 2 ? 32 : 16);
+  static constexpr int kV = KT * kPitch, kBytes = kV + KT * kVPitch;
+  __device__ static inline int k_off(int row, int e) { return row * kPitch + e * EB; }
+  __device__ static inline int v_off(int row, int e) { return kV + row * kVPitch + e * EB; }
+  __device__ static inline void put(char* st, bool v, int row, int e, const uint4& w) {
+    *reinterpret_cast<uint4*>(st + (v ? v_off(row, e) : k_off(row, e))) = w;
+  }
 };
 
 // One wave's share (of NW waves) of a KT-key tile of K and V, in registers. A
 // load instruction covers R whole rows; pages hold 16 tokens or more, so 16 rows
 // lie in one page and have one scalar address.
-template <typename T, int D, int KT, bool F8, int NW>
+template <typename T, int D, typename ST, bool F8, int NW>
 struct TileRegs {
-  using TL = Tile<T, D>;
-  using ST = Stage<T, D, KT>;
+  static constexpr int KT = ST::KT;
   static constexpr int EB = Elem<T>::kBytes;
   static constexpr int PPR = (F8 ? D : D * EB) / 16;  // 16-byte pieces of a held row
   static constexpr int R = 64 / PPR;
@@ -277,14 +324,32 @@ struct TileRegs {
   static constexpr int IPB = 16 / R;                  // instructions per 16 rows
   static constexpr int PE = F8 ? 16 : 16 / EB;        // elements of a piece
   static_assert(IPW % IPB == 0, "a wave loads whole blocks of 16 rows");
+  static constexpr int BLOCKS = NW == 1 ? KT / 16 : 1;  // blocks of 16 rows of a tensor that the wave loads
   u32x4 w[IPW];
+  uint32_t sc;  // F8, NW == 1: scale byte of K's row `lane`, or V's row lane - KT; else of the wave's row lane % 16
 
-  __device__ inline void load(const KvItem& a, int tile, int page, int wave, int lane) {
+  // `page`: of the wave's blocks.
+  __device__ inline void load(const KvItem& a, int tile, const int (&page)[BLOCKS], int wave, int lane) {
+    if constexpr (F8) {
+      const uint32_t low = (uint32_t)page[0], high = (uint32_t)page[BLOCKS - 1];
+      uint32_t pg = low, row;
+      const uint8_t* base;
+      if constexpr (NW == 1) {
+        static_assert(KT == 32, "K's and V's scales fill a wave");
+        row = lane & 31;
+        pg = row & 16 ? high : low;
+        base = lane & 32 ? a.v_scale : a.k_scale;
+      } else {
+        row = (wave * IPW % NI) * R + (lane & 15);
+        base = wave * IPW >= NI ? a.v_scale : a.k_scale;
+      }
+      sc = base[(uint64_t)pg * a.scale_page + (uint32_t)((tile * KT + row) & a.mask)];
+    }
 #pragma unroll
     for (int b = 0; b < IPW / IPB; ++b) {
       const int j = wave * IPW + b * IPB, row = (j % NI) * R;
       const bool v = j >= NI;
-      const uint32_t pg = (uint32_t)__builtin_amdgcn_readlane(page, row), slot = (uint32_t)((tile * KT + row) & a.mask);
+      const uint32_t pg = (uint32_t)page[NW == 1 ? b % BLOCKS : 0], slot = (uint32_t)((tile * KT + row) & a.mask);
       const uint32_t tok = v ? a.v_tok : a.k_tok;
       const char* base = (v ? a.v : a.k) + ((uint64_t)pg * (v ? a.v_page : a.k_page) + (uint64_t)slot * tok);
 #pragma unroll
@@ -294,61 +359,92 @@ struct TileRegs {
   }
 
   // Into the LDS stage. masked: rows that are not ok are zeros, and what is not
-  // finite in V is left out; returns the rows of V that have such elements.
-  __device__ inline uint64_t store(char* st, const TileKeys<KT>& k, bool masked, int wave, int lane) const {
-    uint64_t bad = 0;
+  // finite in V is left out; returns whether there was such in the wave's rows.
+  __device__ __forceinline__ bool store(char* st, uint64_t ok_rows, bool masked, int wave, int lane) const {
+    if (masked) return put<true>(st, ok_rows, wave, lane);
+    return put<false>(st, ok_rows, wave, lane);
+  }
+  template <bool MASKED>
+  __device__ __forceinline__ bool put(char* st, uint64_t ok_rows, int wave, int lane) const {
+    bool bad = false;
 #pragma unroll
     for (int i = 0; i < IPW; ++i) {
       const int j = wave * IPW + i, row0 = (j % NI) * R, row = row0 + lane / PPR;
       const bool v = j >= NI;
       uint4 out[PE * EB / 16];
       if constexpr (F8) {
-        const float sc = __uint_as_float((uint32_t)__shfl((int)(v ? k.vs : k.ks), row, 64) << 23);
+        const int from = NW == 1 ? (v ? KT : 0) + row : row & 15;
+        const float scale = __uint_as_float((uint32_t)__shfl((int)sc, from, 64) << 23);
 #pragma unroll
         for (int o = 0; o < PE * EB / 16; ++o) {
           uint32_t c[Codes<T>::kWords];
 #pragma unroll
           for (int x = 0; x < Codes<T>::kWords; ++x) c[x] = w[i][o * Codes<T>::kWords + x];
-          out[o] = Codes<T>::decode(c, sc);
+          out[o] = Codes<T>::decode(c, scale);
         }
       } else {
         out[0] = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
       }
-      if (masked) {
-        const bool ok = (k.ok >> row) & 1;
-        bool fine = true;
+      if constexpr (MASKED) {
+        const bool ok = (ok_rows >> row) & 1;
 #pragma unroll
         for (int o = 0; o < PE * EB / 16; ++o) {
           if (!ok) out[o] = make_uint4(0u, 0u, 0u, 0u);
           if (v && !finite16<T>(out[o])) {
-            fine = false;
+            bad = true;
             out[o] = only_finite<T>(out[o]);
           }
-        }
-        uint64_t lanes = __ballot(!fine);
-        while (lanes) {
-          const int l = __builtin_ctzll(lanes);
-          lanes &= lanes - 1;
-          bad |= 1ull << (row0 + l / PPR);
         }
       }
 #pragma unroll
       for (int o = 0; o < PE * EB / 16; ++o) {
-        const int e = (lane % PPR) * PE + o * 16 / EB;
-        if (EB == 2 || !v) {
-          *reinterpret_cast<uint4*>(st + (v ? ST::kV : 0) + TL::row_off(row, e)) = out[o];
-        } else {
-          const uint32_t x[4] = {out[o].x, out[o].y, out[o].z, out[o].w};
-          const int kp = kpos_of<Elem<T>::E>(row);
-#pragma unroll
-          for (int y = 0; y < 4; ++y)
-            *reinterpret_cast<uint32_t*>(st + ST::t_off(e + y, kp)) = x[y];
-        }
+        ST::put(st, v, row, (lane % PPR) * PE + o * 16 / EB, out[o]);
       }
     }
-    return bad;
+    if constexpr (MASKED) return __any(bad);
+    return false;
   }
 };
+
+// Element e of a held row of V where it is not finite, else 0.
+template <typename T, bool F8>
+__device__ inline float not_finite(const char* row, int e) {
+  float x;
+  if constexpr (F8) x = (row[e] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
+  else if constexpr (Elem<T>::kBytes == 2) x = bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(row + 2 * e));
+  else x = *reinterpret_cast<const float*>(row + 4 * e);
+  return fabsf(x) < __builtin_inff() ? 0.0f : x;
+}
+
+// What is not finite in V is left out of masked tiles (a product with p = 0
+// would bring it to rows that do not attend its key). Where there was such, the
+// units first, first + stride, ... before `last`, of `sub` tiles each, are looked
+// through again after the loop, and add(position, row) adds it to the rows that do
+// attend it. Rare, and apart from the loop: inside it, it cost the loop its registers.
+template <typename T, int D, int KT, bool F8, typename Add>
+__device__ inline void bad_rows(const KvItem& a, int first, int last, int stride, int sub, int first_pos, int lane, Add&& add) {
+  for (int i = 0, y = first * sub; y < last * sub; i = i + 1 == sub ? 0 : i + 1, y += i ? 1 : (stride - 1) * sub + 1) {
+    const uint64_t ok = present<KT>(a, y, lane);
+    if (ok == all_keys<KT>() && y * KT + KT - 1 <= first_pos) continue;  // not masked
+    bool fine = true;
+    if ((ok >> lane) & 1) {  // a row per lane
+      const char* row = a.v_row(y * KT + lane);
+      for (int e = 0; e < D; ++e) fine = fine && not_finite<T, F8>(row, e) == 0.0f;
+    }
+    uint64_t bad = __ballot(!fine);
+    while (bad) {
+      const int t = y * KT + __builtin_ctzll(bad);
+      bad &= bad - 1;
+      add(t, a.v_row(t));
+    }
+  }
+}
+
+// Folded row f of kv head h of the sequence whose rows begin at `first`.
+__device__ inline const char* query_row(const PagedAttnArgs& a, int first, int h, int64_t f) {
+  const int hq = (h << a.gqa_shift) + (int)(f & ((1 << a.gqa_shift) - 1));
+  return row_ptr(a.Q, first + (f >> a.gqa_shift), a.q_tok) + hq * a.q_head;
+}
 
 // ---------------------------------------------------------------- one wave's rows
 
@@ -374,12 +470,9 @@ struct WaveRows {
   __device__ inline void begin(const PagedAttnArgs& a, const Q& q, int h, int64_t f0, int lane) {
     const int hh = lane >> 5;
     const int64_t nf = (int64_t)q.n << a.gqa_shift;
-    int64_t f = f0 + (lane & 31);
+    const int64_t f = f0 + (lane & 31);
     pos = f < nf ? q.pos(f >> a.gqa_shift) : -1;
-    if (f >= nf) f = nf - 1;
-    const int64_t row = q.first + (f >> a.gqa_shift);
-    const int hq = (h << a.gqa_shift) + (int)(f & ((1 << a.gqa_shift) - 1));
-    const char* p = row_ptr(a.Q, row, a.q_tok) + hq * a.q_head;
+    const char* p = query_row(a, q.first, h, f < nf ? f : nf - 1);
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) qf[ks] = EL::load_frag(p + (ks * KS + E * hh) * EB);
 #pragma unroll
@@ -388,95 +481,155 @@ struct WaveRows {
     l = 0.0f;
   }
 
-  // One tile from its LDS stage. masked: keys that are not ok or after the row do not count.
-  __device__ __forceinline__ void step(const char* st, int tile, uint64_t ok, bool masked, float c, int lane) {
-    const int hh = lane >> 5, l32 = lane & 31;
-    const float lazy = 8.0f / c;
-    f32x16 s[NH];
+  using Probs = Frag[VPS];  // P of 32 keys, as the operand of P.V
+
+  // Raw scores of keys 32 t ... of the stage.
+  __device__ __forceinline__ void scores(f32x16& s, const char* st, int t, int lane) const {
+    s = f32x16{};
 #pragma unroll
-    for (int t = 0; t < NH; ++t) s[t] = f32x16{};
-#pragma unroll
-    for (int t = 0; t < NH; ++t)
-#pragma unroll
-      for (int ks = 0; ks < NKS; ++ks) {
-        const Frag kf = EL::load_frag(st + TL::row_off(32 * t + l32, ks * KS + E * hh));
-        s[t] = EL::mma(kf, qf[ks], s[t]);
-      }
-    if (masked) {
-      const int rel = pos < 0 ? -1 : pos - tile * KT;  // keys 0 .. rel are at or before the row
-      const uint64_t see = (ok & (rel < 0 ? 0 : rel >= 63 ? ~0ull : (2ull << rel) - 1)) >> (4 * hh);
-#pragma unroll
-      for (int t = 0; t < NH; ++t)
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (!((see >> (32 * t + 8 * (v >> 2) + (v & 3))) & 1)) s[t][v] = -__builtin_inff();
+    for (int ks = 0; ks < NKS; ++ks) {
+      const Frag kf = EL::load_frag(st + TL::row_off(32 * t + (lane & 31), ks * KS + E * (lane >> 5)));
+      s = EL::mma(kf, qf[ks], s);
     }
+  }
+  // Keys of them that are not ok or after the row do not count.
+  __device__ __forceinline__ void hide(f32x16& s, int tile, int t, uint64_t ok, int lane) const {
+    const int rel = pos < 0 ? -1 : pos - tile * KT;  // keys 0 .. rel are at or before the row
+    const uint64_t see = ok & (rel < 0 ? 0 : rel >= 63 ? ~0ull : (2ull << rel) - 1);
+    const uint32_t mine = (uint32_t)(see >> (32 * t)) >> (4 * (lane >> 5));
 #pragma unroll
-    for (int t = 0; t < NH; ++t) {
-      float mx = -__builtin_inff();
+    for (int v = 0; v < 16; ++v)
+      if (!((mine >> (8 * (v >> 2) + (v & 3))) & 1)) s[v] = -__builtin_inff();
+  }
+  __device__ __forceinline__ static float row_max(const f32x16& s) {
+    float mx = s[0];
 #pragma unroll
-      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[t][v]);
-      mx = half_max(mx);
-      const bool raise = mx > m + lazy;  // the first finite score too: m = -inf
-      if (__any(raise)) {
-        const float mn = raise ? mx : m;
-        const float corr = raise ? __builtin_amdgcn_exp2f((m - mn) * c) : 1.0f;
-        m = mn;
-        l *= corr;
+    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
+    return half_max(mx);
+  }
+  // The running maximum follows mx, O and the sum with it, where it grew by over 2^8.
+  __device__ __forceinline__ void raise(float mx, float c) {
+    const bool up = mx > m + 8.0f / c;  // the first finite score too: m = -inf
+    if (__any(up)) {
+      const float mn = up ? mx : m;
+      const float corr = up ? __builtin_amdgcn_exp2f((m - mn) * c) : 1.0f;
+      m = mn;
+      l *= corr;
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) oacc[dt] *= corr;
+      for (int dt = 0; dt < NDT; ++dt) oacc[dt] *= corr;
+    }
+  }
+  __device__ __forceinline__ void probs(const f32x16& s, Probs& pf, float c) {
+    const float mc = m == -__builtin_inff() ? 0.0f : m * c;  // nothing attended yet: every p is 0
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < VPS; ++k) {
+      float pv[E];
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        pv[j] = __builtin_amdgcn_exp2f(fmaf(s[E * k + j], c, -mc));
+        sum += pv[j];
       }
-      const float mc = m == -__builtin_inff() ? 0.0f : m * c;  // nothing attended yet: every p is 0
-      float sum = 0.0f;
+      pf[k] = EL::frag_from(pv);  // bf16: P is rounded to the inputs' precision, as in the routed forward
+    }
+    l += sum;
+  }
+  // O^T += V^T . P^T over keys 32 t ... of the stage.
+  __device__ __forceinline__ void values(const Probs& pf, const char* st, int t, int lane) {
+    const int hh = lane >> 5, l32 = lane & 31;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        s[t][v] = __builtin_amdgcn_exp2f(fmaf(s[t][v], c, -mc));
-        sum += s[t][v];
-      }
-      l += sum;
+    for (int k = 0; k < VPS; ++k) {
+      const int kk = t * VPS + k;
 #pragma unroll
-      for (int s2 = 0; s2 < VPS; ++s2) {
-        const int k = t * VPS + s2;
-        float pv[E];
-#pragma unroll
-        for (int j = 0; j < E; ++j) pv[j] = s[t][E * s2 + j];
-        const Frag pf = EL::frag_from(pv);  // bf16: P is rounded to the inputs' precision, as in the routed forward
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) {
-          Frag vf;
-          if constexpr (ST::TR) vf = tr_frag<TL>(st + ST::kV, 32 * dt, 16 * k + 4 * hh, 16 * k + 8 + 4 * hh, lane);
-          else vf = EL::load_frag(st + ST::t_off(32 * dt + l32, KS * k + E * hh));
-          oacc[dt] = EL::mma(vf, pf, oacc[dt]);
-        }
+      for (int dt = 0; dt < NDT; ++dt) {
+        Frag vf;
+        if constexpr (ST::TR) vf = tr_frag<TL>(st + ST::kV, 32 * dt, 16 * kk + 4 * hh, 16 * kk + 8 + 4 * hh, lane);
+        else vf = EL::load_frag(st + ST::t_off(32 * dt + l32, KS * kk + E * hh));
+        oacc[dt] = EL::mma(vf, pf[k], oacc[dt]);
       }
     }
   }
 
-  // What is not finite in V was left out of the tile (a product with p = 0
-  // would bring it to rows that do not attend its key): added here to the
-  // rows that do.
+  // Operands of the products to come: the next four steps' (see half()).
+  static constexpr int RING = 4, NB = NDT * VPS;
+  __device__ __forceinline__ static Frag k_frag(const char* st, int t, int ks, int lane) {
+    return EL::load_frag(st + TL::row_off(32 * t + (lane & 31), ks * KS + E * (lane >> 5)));
+  }
+  __device__ __forceinline__ static Frag v_frag(const char* st, int t, int i, int lane) {
+    const int kk = t * VPS + i / NDT, hh = lane >> 5;
+    return tr_frag<TL>(st + ST::kV, 32 * (i % NDT), 16 * kk + 4 * hh, 16 * kk + 8 + 4 * hh, lane);
+  }
+
+  // bf16: 32 keys whose scores are in s (V: half t of stage st), beside the
+  // scores sn of the 32 after them (K: half tn of stage stn; MORE: there are
+  // such). NKS + NB steps of one product each. The product's operand was read
+  // from LDS four steps ahead; beside the first NKS products go the
+  // exponentials, beside the others the maximum of sn. The order is fixed by
+  // hand: left to itself the compiler gathers the products and waits for each operand
+  // right after asking for it. fr holds the first operands on entry, and those of the
+  // next call on return, whose K is half tk of stage stk.
+  template <bool MORE, typename Hide>
+  __device__ __forceinline__ void half(f32x16& s, f32x16& sn, Frag (&fr)[RING], const char* st, int t, const char* stn,
+                                       int tn, const char* stk, int tk, float c, int lane, Hide&& hide_next) {
+    const float mc = m == -__builtin_inff() ? 0.0f : m * c;  // nothing attended yet: every p is 0
+    float sum = 0.0f;
+    Probs pf;
+    constexpr int PER = 16 / NKS;
+#pragma unroll
+    for (int i = 0; i < NKS; ++i) {
+      if constexpr (MORE) sn = EL::mma(fr[i % RING], qf[i], i == 0 ? f32x16{} : sn);
+      const int next = i + RING;
+      if (next >= NKS) fr[i % RING] = v_frag(st, t, next - NKS, lane);
+      else if constexpr (MORE) fr[i % RING] = k_frag(stn, tn, next, lane);
+#pragma unroll
+      for (int j = i * PER; j < (i + 1) * PER; ++j) {
+        s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], c, -mc));
+        sum += s[j];
+      }
+      if ((i + 1) * PER % E == 0) {  // bf16: P is rounded to the inputs' precision, as in the routed forward
+        const int k = ((i + 1) * PER - 1) / E;
+        float pv[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) pv[j] = s[E * k + j];
+        pf[k] = EL::frag_from(pv);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    l += sum;
+#pragma unroll
+    for (int k = 0; k < VPS; ++k) asm volatile("" : "+v"(pf[k]));  // here, and not past the branch
+    hide_next();
+    float mx = -__builtin_inff();
+    constexpr int MAXES = 16 / (NB / 2);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      oacc[i % NDT] = EL::mma(fr[(NKS + i) % RING], pf[i / NDT], oacc[i % NDT]);
+      const int next = i + RING;
+      if (next < NB) fr[(NKS + i) % RING] = v_frag(st, t, next, lane);
+      else if constexpr (MORE) fr[(NKS + i) % RING] = k_frag(stk, tk, next - NB, lane);
+      if constexpr (MORE) {
+        if (i >= NB / 2) {
+#pragma unroll
+          for (int j = (i - NB / 2) * MAXES; j < (i - NB / 2 + 1) * MAXES; ++j) mx = fmaxf(mx, sn[j]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (MORE) raise(half_max(mx), c);
+  }
+
   template <bool F8>
-  __device__ inline void add_bad(const KvItem& a, int tile, uint64_t bad, int lane) {
-    const int hh = lane >> 5;
-    while (bad) {
-      const int kk = __builtin_ctzll(bad);
-      bad &= bad - 1;
-      const int t = tile * KT + kk;
-      if (pos < t) continue;
-      const char* row = a.v + page_off(a.table[t >> a.shift], t & a.mask, a.v_page, a.v_tok);  // a row of the tile: present
+  __device__ inline void add_bad(const KvItem& a, int first, int last, int first_pos, int lane) {
+    bad_rows<T, D, KT, F8>(a, first, last, 1, 1, first_pos, lane, [&](int t, const char* row) {
+      if (pos < t) return;
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          const int d = 32 * dt + 8 * (v >> 2) + 4 * hh + (v & 3);
-          float x;
-          if constexpr (F8) x = (row[d] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
-          else if constexpr (EB == 2) x = bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(row + 2 * d));
-          else x = *reinterpret_cast<const float*>(row + 4 * d);
-          if (!(fabsf(x) < __builtin_inff())) oacc[dt][v] += x;
-          __builtin_amdgcn_sched_barrier(0);  // one at a time: all at once, the comparisons take the loops' scalars
+          oacc[dt][v] += not_finite<T, F8>(row, 32 * dt + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3));
+          __builtin_amdgcn_sched_barrier(0);
         }
-    }
+    });
   }
 };
 
@@ -534,108 +687,278 @@ __device__ inline void walk(Share<KS> sh, int wg, int shift, F&& f) {
 
 }  // namespace
 
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+
+namespace {
+
 // ---------------------------------------------------------------- few rows
 
-// Up to 32 folded rows per item: the four waves take every fourth tile each,
+// 16x16 products (lane l, quarter q = l / 16): A row and B column l % 16, k = E q + j; C
+// column l % 16, row 4 q + v. bf16: k = 32, E = 8; float32: k = 4, E = 1.
+template <typename T> struct Elem16;
+template <> struct Elem16<__bf16> {
+  using Frag = bf16x8;
+  static constexpr int E = 8, KS = 32;
+  __device__ static inline f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Elem16<float> {
+  using Frag = float;
+  static constexpr int E = 1, KS = 4;
+  __device__ static inline f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+};
+
+// NR groups of 16 folded rows: lane l holds (a quarter of the head dim of) row
+// l % 16 of each. A 32-key tile's scores are two 16x16 tiles: of row l % 16 the lane has
+// keys 4 q + v and 16 + 4 q + v, which in that order are P's operand.
+template <typename T, int D, int NR>
+struct FewRows {
+  using EL = Elem16<T>;
+  using Frag = typename EL::Frag;
+  using ST = FewStage<T, D>;
+  static constexpr int E = EL::E, KS = EL::KS, EB = Elem<T>::kBytes, NKS = D / KS, NDT = D / 16;
+
+  Frag qf[NR][NKS];
+  f32x4 oacc[NR][NDT];
+  float m[NR], l[NR];
+  int pos[NR];
+
+  template <typename Q>
+  __device__ inline void begin(const PagedAttnArgs& a, const Q& q, int h, int64_t f0, int lane) {
+    const int64_t nf = (int64_t)q.n << a.gqa_shift;
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      const int64_t f = f0 + 16 * r + (lane & 15);
+      pos[r] = f < nf ? q.pos(f >> a.gqa_shift) : -1;
+      const char* p = query_row(a, q.first, h, f < nf ? f : nf - 1);
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) qf[r][ks] = *reinterpret_cast<const Frag*>(p + (ks * KS + E * (lane >> 4)) * EB);
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) oacc[r][dt] = f32x4{};
+      m[r] = -__builtin_inff();
+      l[r] = 0.0f;
+    }
+  }
+
+  // A 32-key tile from its LDS stage. masked: keys that are not ok or after the row do not count.
+  __device__ __forceinline__ void step(const char* st, int tile, uint64_t ok, bool masked, float c, int lane) {
+    const int q = lane >> 4, l16 = lane & 15;
+    f32x4 s[NR][2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r) s[r][t] = f32x4{};
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) {
+        const Frag kf = *reinterpret_cast<const Frag*>(st + ST::k_off(16 * t + l16, ks * KS + E * q));
+#pragma unroll
+        for (int r = 0; r < NR; ++r) s[r][t] = EL::mma(kf, qf[r][ks], s[r][t]);
+      }
+    }
+    if (masked) {
+      asm volatile("");  // a branch, not selects in every tile
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        const int rel = pos[r] < 0 ? -1 : pos[r] - tile * 32;  // keys 0 .. rel are at or before the row
+        const uint32_t see = ((uint32_t)ok & (rel < 0 ? 0u : rel >= 31 ? ~0u : (2u << rel) - 1)) >> (4 * q);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (!((see >> (16 * t + v)) & 1)) s[r][t][v] = -__builtin_inff();
+      }
+    }
+    Frag pf[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      float mx = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])),
+                       fmaxf(fmaxf(s[r][1][0], s[r][1][1]), fmaxf(s[r][1][2], s[r][1][3])));
+      float other = mx;
+      swap16(mx, other);
+      mx = half_max(fmaxf(mx, other));
+      const bool up = mx > m[r] + 8.0f / c;  // the first finite score too: m = -inf
+      if (__any(up)) {
+        const float mn = up ? mx : m[r];
+        const float corr = up ? __builtin_amdgcn_exp2f((m[r] - mn) * c) : 1.0f;
+        m[r] = mn;
+        l[r] *= corr;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) oacc[r][dt] *= corr;
+      }
+      const float mc = m[r] == -__builtin_inff() ? 0.0f : m[r] * c;  // nothing attended yet: every p is 0
+      float sum = 0.0f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          s[r][t][v] = __builtin_amdgcn_exp2f(fmaf(s[r][t][v], c, -mc));
+          sum += s[r][t][v];
+        }
+      l[r] += sum;
+      if constexpr (EB == 2)  // P is rounded to the inputs' precision, as in the routed forward
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pf[r][j] = (__bf16)s[r][j >> 2][j & 3];
+    }
+    if constexpr (EB == 2) {
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        typedef __attribute__((address_space(3))) s16x4* lds_s4;
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        const char* p = st + ST::v_off(4 * q + (l16 >> 2), 16 * dt + 4 * (l16 & 3));
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)p);
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(p + 16 * ST::kVPitch));
+        const Frag vf = __builtin_bit_cast(Frag, (s16x8)__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int r = 0; r < NR; ++r) oacc[r][dt] = EL::mma(vf, pf[r], oacc[r][dt]);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt) {
+            const float vf = *reinterpret_cast<const float*>(st + ST::v_off(16 * t + 4 * q + v, 16 * dt + l16));
+#pragma unroll
+            for (int r = 0; r < NR; ++r) oacc[r][dt] = EL::mma(vf, s[r][t][v], oacc[r][dt]);
+          }
+    }
+  }
+
+  template <bool F8>
+  __device__ inline void add_bad(const KvItem& a, int first, int last, int stride, int sub, int first_pos, int lane) {
+    bad_rows<T, D, 32, F8>(a, first, last, stride, sub, first_pos, lane, [&](int t, const char* row) {
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float x = not_finite<T, F8>(row, 16 * dt + 4 * (lane >> 4) + v);
+#pragma unroll
+          for (int r = 0; r < NR; ++r) oacc[r][dt][v] += pos[r] < t ? 0.0f : x;
+        }
+    });
+  }
+};
+
+}  // namespace
+
+// Up to 16 NR folded rows per item: the four waves take every fourth unit each,
 // on the same rows, with LDS of their own and no barrier; their results are
-// joined at the item's end. 32-key tiles, so that two workgroups fit a CU and
-// one's rows are under way while the other begins or ends an item. 8-bit rows
-// are asked for two tiles ahead, which keeps as many bytes under way as one of
-// bf16 rows does (16 KB a wave, 128 KB a CU).
-template <typename T, int D, bool F8>
+// joined at the item's end. Tiles of 32 keys, so that two workgroups fit a CU and
+// one's rows are under way while the other begins or ends an item. A unit is a
+// tile, or two of 8-bit rows, whose loads are under way at once: either way 16 KB a
+// wave and 128 KB a CU, about what the memory's latency takes. 16-row products
+// although the matrix cores have time to spare: it is the instructions beside them that
+// count (with 32 rows, 64 ragged contexts in 8 bits 180 us).
+template <typename T, int D, bool F8, int NR>
 __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs) {
-  constexpr int KT = 1 << kPagedFewKeys, NW = 4, OP = D + 4, DEPTH = F8 ? 2 : 1;
-  using W = WaveRows<T, D, KT>;
-  constexpr int SB = W::ST::kBytes > 32 * OP * 4 ? W::ST::kBytes : 32 * OP * 4;  // a wave's LDS: a stage, then its results
+  constexpr int UK = few_unit_keys(F8), SUB = (1 << UK) / 32, KT = 32, NW = 4, M = 16 * NR, OP = D + 4;
+  using W = FewRows<T, D, NR>;
+  constexpr int SB = W::ST::kBytes > M * OP * 4 ? W::ST::kBytes : M * OP * 4;  // a wave's LDS: a stage, then its results
   __shared__ __attribute__((aligned(16))) char smem[NW * SB];
-  __shared__ float s_m[NW][32], s_l[NW][32];
+  __shared__ float s_m[NW][M], s_l[NW][M];
   __shared__ int64_t s_scan[NW + 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int shift = kPagedFewRowsLog2 - args_here().gqa_shift, wg = share_index();
-  const Share<kPagedFewKeys> share = take_share<256, kPagedFewWorkgroups, kPagedFewKeys>(wg, shift, NW, NW, s_scan);
+  const int shift = (NR == 1 ? 4 : 5) - args_here().gqa_shift, wg = share_index();
+  const Share<UK> share = take_share<256, kPagedFewWorkgroups, UK>(wg, shift, NW, NW, s_scan);
   const float c = args_here().scale_log2;
   char* st = smem + wave * SB;
-  walk(share, wg, shift, [&](const Share<kPagedFewKeys>& sh, int n, bool whole) {
-    const SeqShape<kPagedFewKeys>& q = sh.q;
+  walk(share, wg, shift, [&](const Share<UK>& sh, int n, bool whole) {
+    const SeqShape<UK>& q = sh.q;
     const PagedAttnArgs& a0 = args_here();
     const int first_pos = q.pos((int64_t)sh.j << shift);
     const KvItem kv(a0.p, sh.s, sh.h, q.end(sh.j));
     W w;
-    w.begin(a0, q, sh.h, (int64_t)sh.j * kPagedFewRows, lane);
-    const int last = sh.kt + n;
-    int x = sh.kt + wave;
-    // slot i holds a tile's rows and keys; `next` the pages of the one to ask for next
-    TileRegs<T, D, KT, F8, 1> r[DEPTH];
-    TileKeys<KT> key[DEPTH], next;
-    auto ask = [&](int i, int y) __attribute__((always_inline)) {
-      key[i].entry = next.entry;
-      key[i].use(kv);
-      next.ask(kv, y + NW, lane);
-      key[i].template ask_scales<F8>(kv, y, lane);
-      r[i].load(kv, y, key[i].page, 0, lane);
-    };
-    next.ask(kv, x, lane);
-#pragma unroll
-    for (int i = 0; i < DEPTH; ++i)
-      if (x + i * NW < last) ask(i, x + i * NW);
-    while (x < last) {
-#pragma unroll
-      for (int i = 0; i < DEPTH; ++i) {
-        if (x >= last) break;
-        // positions after the first row lie in this tile, or some are not there
-        const uint64_t ok = key[i].ok;
-        const bool masked = x * KT + KT - 1 > first_pos || ok != key[i].kAll;
-        const uint64_t bad = r[i].store(st, key[i], masked, 0, lane);
-        __builtin_amdgcn_wave_barrier();
-        if (x + DEPTH * NW < last) ask(i, x + DEPTH * NW);
-        w.step(st, x, ok, masked, c, lane);
-        if (bad) w.template add_bad<F8>(kv, x, bad, lane);
-        __builtin_amdgcn_wave_barrier();
-        x += NW;
+    w.begin(a0, q, sh.h, (int64_t)sh.j * M, lane);
+    const int last = sh.kt + n, x0 = sh.kt + wave;
+    // slot i holds the rows of unit x's tile i; `map` the pages of the units to ask for
+    TileRegs<T, D, typename W::ST, F8, 1> r[SUB];
+    TileMap<(1 << UK), NW, 2 * SUB> map;
+    bool full_now = false, full = false, bad = false;  // of unit x, and of the one asked for
+    int x = x0, at = 0;
+    auto ask = [&](int i, int u) __attribute__((always_inline)) {  // tile i of unit u
+      if (i == 0) {
+        if (at == 0) map.fill(kv, u, 0, lane);
+        full = (map.full >> at) & 1;
       }
+      const int page[2] = {__builtin_amdgcn_readlane(map.page[2 * i], at), __builtin_amdgcn_readlane(map.page[2 * i + 1], at)};
+      r[i].load(kv, u * SUB + i, page, 0, lane);
+      if (i == SUB - 1) at = (at + 1) & 63;
+    };
+    auto tile = [&](int i, auto more) __attribute__((always_inline)) {
+      // positions after the first row lie in this tile, or some are not there
+      const int y = x * SUB + i;
+      uint64_t ok = ~0ull;
+      bool masked = y * KT + KT - 1 > first_pos;
+      if (!full_now) {  // of the unit: this tile may be
+        ok = present<KT>(kv, y, lane);
+        masked = masked || ok != all_keys<KT>();
+      }
+      bad = r[i].store(st, ok, masked, 0, lane) || bad;
+      __builtin_amdgcn_wave_barrier();
+      if constexpr (more.value) ask(i, x + NW);
+      w.step(st, y, ok, masked, c, lane);
+      __builtin_amdgcn_wave_barrier();
+    };
+    if (x < last) {
+#pragma unroll
+      for (int i = 0; i < SUB; ++i) ask(i, x);
+      // The last unit apart: where a slot may or may not be asked for again, the
+      // compiler waits for both before it takes either.
+      for (; x + NW < last; x += NW) {
+        full_now = full;
+#pragma unroll
+        for (int i = 0; i < SUB; ++i) tile(i, Yes());
+      }
+      full_now = full;
+#pragma unroll
+      for (int i = 0; i < SUB; ++i) tile(i, No());
     }
+    if (bad) w.template add_bad<F8>(kv, x0, last, NW, SUB, first_pos, lane);
     // join the waves: rows as [wave][row][D] through the stages
     const PagedAttnArgs& a = args_here();
-    const float l = half_sum(w.l);
     __syncthreads();
     float* so = reinterpret_cast<float*>(smem);
-    const int hh = lane >> 5, l32 = lane & 31;
-    if (hh == 0) {
-      s_m[wave][l32] = w.m;
-      s_l[wave][l32] = l;
+    const int q4 = lane >> 4, l16 = lane & 15;
+#pragma unroll
+    for (int g = 0; g < NR; ++g) {
+      float l = w.l[g], other = l;
+      swap16(l, other);
+      l = half_sum(l + other);
+      if (q4 == 0) {
+        s_m[wave][16 * g + l16] = w.m[g];
+        s_l[wave][16 * g + l16] = l;
+      }
+#pragma unroll
+      for (int dt = 0; dt < W::NDT; ++dt)
+        *reinterpret_cast<f32x4*>(so + (wave * M + 16 * g + l16) * OP + 16 * dt + 4 * q4) = w.oacc[g][dt];
     }
-#pragma unroll
-    for (int dt = 0; dt < W::NDT; ++dt)
-#pragma unroll
-      for (int v4 = 0; v4 < 4; ++v4)
-        *reinterpret_cast<f32x4*>(so + (wave * 32 + l32) * OP + 32 * dt + 8 * v4 + 4 * hh) =
-            f32x4{w.oacc[dt][4 * v4], w.oacc[dt][4 * v4 + 1], w.oacc[dt][4 * v4 + 2], w.oacc[dt][4 * v4 + 3]};
     __syncthreads();
-    const int64_t nf = (int64_t)q.n << a.gqa_shift, f0 = (int64_t)sh.j * kPagedFewRows;
-    const int rows = nf - f0 < kPagedFewRows ? (int)(nf - f0) : kPagedFewRows;
+    const int64_t nf = (int64_t)q.n << a.gqa_shift, f0 = (int64_t)sh.j * M;
+    const int rows = nf - f0 < M ? (int)(nf - f0) : M;
     const int64_t slot = (int64_t)wg * 2 + (sh.kt == 0 ? 1 : 0);
     for (int it = tid; it < rows * (D / 4); it += 256) {
       const int row = it / (D / 4), d4 = it % (D / 4);
-      float M = -__builtin_inff();
+      float mx = -__builtin_inff();
 #pragma unroll
-      for (int k = 0; k < NW; ++k) M = fmaxf(M, s_m[k][row]);
+      for (int k = 0; k < NW; ++k) mx = fmaxf(mx, s_m[k][row]);
       float L = 0.0f;
       f32x4 o = f32x4{};
 #pragma unroll
       for (int k = 0; k < NW; ++k) {
-        const float f = s_m[k][row] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((s_m[k][row] - M) * c);
+        const float f = s_m[k][row] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((s_m[k][row] - mx) * c);
         L += s_l[k][row] * f;
-        o += *reinterpret_cast<const f32x4*>(so + (k * 32 + row) * OP + 4 * d4) * f;
+        o += *reinterpret_cast<const f32x4*>(so + (k * M + row) * OP + 4 * d4) * f;
       }
       if (whole) {
         float* lse;
         char* dst = out_row(a, q.first, sh.h, f0 + row, lse);
         store4(dst + d4 * 4 * W::EB, o * (L == 0.0f ? 0.0f : 1.0f / L), W::EB == 2);
-        if (d4 == 0) *lse = lse_of(M, L, c);
+        if (d4 == 0) *lse = lse_of(mx, L, c);
       } else {
         *reinterpret_cast<f32x4*>(a.part + (slot * a.slot_rows + row) * D + 4 * d4) = o;
         if (d4 == 0) {
-          a.part_ml[(slot * a.slot_rows + row) * 2] = M;
+          a.part_ml[(slot * a.slot_rows + row) * 2] = mx;
           a.part_ml[(slot * a.slot_rows + row) * 2 + 1] = L;
         }
       }
@@ -646,20 +969,28 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs) {
 
 // ---------------------------------------------------------------- many rows
 
-// 256 folded rows per item, 32 per wave; the waves share each tile, which is
-// staged in LDS while the one before it is computed.
+// 256 folded rows per item, 32 per wave; the waves share each tile through three
+// LDS stages. A wave works on 32 keys at a time, in two phases that keep the
+// matrix cores and the vector unit busy at once: the next 32 keys' scores beside
+// these' exponentials, then these' P.V beside the next maximum. Tile x + 1 is
+// staged before tile x is begun, so the phases run on across tiles; x + 2 goes
+// to the third stage meanwhile.
 template <typename T, int D, bool F8>
 __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
   constexpr int KT = 1 << kPagedTileKeys, NW = 8;
   using W = WaveRows<T, D, KT>;
+  using Frag = typename W::Frag;
   constexpr int SB = W::ST::kBytes;
-  __shared__ __attribute__((aligned(16))) char smem[2 * SB];
+  __shared__ __attribute__((aligned(16))) char smem[3 * SB];
   __shared__ int64_t s_scan[NW + 2];
-  __shared__ uint64_t s_bad[2][NW];
+  __shared__ int s_bad[2];  // whether V had what is not finite in this item, and in the next
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int shift = kPagedTileRowsLog2 - args_here().gqa_shift, wg = share_index();
   const Share<kPagedTileKeys> share = take_share<512, kPagedTileWorkgroups, kPagedTileKeys>(wg, shift, 1, 4, s_scan);
   const float c = args_here().scale_log2;
+  if (tid < 2) s_bad[tid] = 0;
+  __syncthreads();
+  int item = 0;
   walk(share, wg, shift, [&](const Share<kPagedTileKeys>& sh, int n, bool whole) {
     const SeqShape<kPagedTileKeys>& q = sh.q;
     const PagedAttnArgs& a0 = args_here();
@@ -668,54 +999,100 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
     const int64_t nf = (int64_t)q.n << a0.gqa_shift, f0 = (int64_t)sh.j * kPagedTileRows + 32 * wave;
     W w;
     w.begin(a0, q, sh.h, f0, lane);
-    // the wave's rows lie at positions wave_first .. wave_last; none if f0 >= nf
-    const int64_t f1 = f0 + 31 < nf ? f0 + 31 : nf - 1;
-    const int wave_first = q.pos(f0 >> a0.gqa_shift), wave_last = f0 < nf ? q.pos(f1 >> a0.gqa_shift) : -1;
+    const bool active = f0 < nf;  // else the wave only stages
+    const int wave_first = q.pos(f0 >> a0.gqa_shift);
     const int last = sh.kt + n;
     int x = sh.kt;
-    TileRegs<T, D, KT, F8, NW> r;
-    TileKeys<KT> cur, nxt;
-    auto ask = [&](int y) {
-      cur.use(kv);
-      nxt.ask(kv, y + 1, lane);
-      cur.template ask_scales<F8>(kv, y, lane);
-      r.load(kv, y, cur.page, wave, lane);
+    TileRegs<T, D, typename W::ST, F8, NW> r;
+    constexpr int IPW = TileRegs<T, D, typename W::ST, F8, NW>::IPW, NI = TileRegs<T, D, typename W::ST, F8, NW>::NI;
+    TileMap<KT, 1, 1> map;
+    const int block = (wave * IPW % NI) * TileRegs<T, D, typename W::ST, F8, NW>::R / 16, x0 = x;
+    int asked = 0;
+    bool full = false;  // of the tile in r
+    auto ask = [&]() __attribute__((always_inline)) {
+      const int at = asked & 63;
+      if (at == 0) map.fill(kv, x0 + asked, block, lane);
+      const int page[1] = {__builtin_amdgcn_readlane(map.page[0], at)};
+      full = (map.full >> at) & 1;
+      r.load(kv, x0 + asked, page, wave, lane);
+      ++asked;
     };
-    cur.ask(kv, x, lane);
-    ask(x);
-    auto put = [&](int tile, const TileKeys<KT>& k) {
-      const bool masked = tile * KT + KT - 1 > first_pos || k.ok != k.kAll;
-      const uint64_t bad = r.store(smem + (tile & 1) * SB, k, masked, wave, lane);
-      if (masked && lane == 0) s_bad[tile & 1][wave] = bad;
+    // stages of tiles x, x + 1, x + 2, and which of their keys are there
+    char *st0 = smem, *st1 = smem + SB, *st2 = smem + 2 * SB;
+    uint64_t ok0, ok1 = 0, ok2 = 0;
+    auto put = [&](int y, char* st, uint64_t& ok) __attribute__((always_inline)) {
+      ok = ~0ull;
+      if (!full) ok = present<KT>(kv, y, lane);
+      const bool masked = y * KT + KT - 1 > first_pos || !full;
+      if (r.store(st, ok, masked, wave, lane)) s_bad[item & 1] = 1;
     };
-    put(x, cur);
-    uint64_t ok = cur.ok;
+    ask();
+    put(x, st0, ok0);
     if (x + 1 < last) {
-      cur = nxt;
-      ask(x + 1);
+      ask();
+      put(x + 1, st1, ok1);
+      if (x + 2 < last) ask();
     }
     __syncthreads();
-    for (; x < last; ++x) {
-      const bool staged = x * KT + KT - 1 > first_pos || ok != cur.kAll;
-      if (x * KT <= wave_last && ok != 0) {  // else no row of the wave attends a key of the tile
-        w.step(smem + (x & 1) * SB, x, ok, x * KT + KT - 1 > wave_first || ok != cur.kAll, c, lane);
-        if (staged) {
-          uint64_t bad = 0;
-#pragma unroll
-          for (int k = 0; k < NW; ++k) bad |= s_bad[x & 1][k];
-          if (bad) w.template add_bad<F8>(kv, x, bad, lane);
-        }
+    if (tid == 0) s_bad[(item + 1) & 1] = 0;  // read after the last item's loop, set in the next one's
+    auto masked = [&](int y, uint64_t ok) { return y * KT + KT - 1 > wave_first || ok != ~0ull; };
+    f32x16 s0, s1;
+    typename W::Probs pf;
+    constexpr Yes yes;
+    constexpr No no;
+    Frag fr[W::RING];
+    // Keys of tile y that do not count, where it has such: a branch (its empty asm
+    // keeps it one; as selects it would run in every tile). With a form of the loop
+    // for tiles without masks the accumulators had two places, and 97 registers went to memory.
+    auto hide = [&](f32x16& s, int y, int t, uint64_t ok) __attribute__((always_inline)) {
+      if (masked(y, ok)) {
+        asm volatile("");
+        w.hide(s, y, t, ok, lane);
       }
-      if (x + 1 < last) {
-        put(x + 1, cur);
-        ok = cur.ok;
-        if (x + 2 < last) {
-          cur = nxt;
-          ask(x + 2);
-        }
+    };
+    // tile x, with the scores of its first half in s0; leaves those of the next tile's
+    auto both = [&](auto more) __attribute__((always_inline)) {
+      auto hide1 = [&]() __attribute__((always_inline)) { hide(s1, x, 1, ok0); };
+      auto hide0 = [&]() __attribute__((always_inline)) { if constexpr (more.value) hide(s0, x + 1, 0, ok1); };
+      if constexpr (sizeof(T) == 2) {
+        w.template half<true>(s0, s1, fr, st0, 0, st0, 1, st1, 0, c, lane, hide1);
+        w.template half<more.value>(s1, s0, fr, st0, 1, st1, 0, st1, 1, c, lane, hide0);
+      } else {
+        w.scores(s1, st0, 1, lane);
+        w.probs(s0, pf, c);
+        hide1();
+        w.values(pf, st0, 0, lane);
+        w.raise(W::row_max(s1), c);
+        if constexpr (more.value) w.scores(s0, st1, 0, lane);
+        w.probs(s1, pf, c);
+        hide0();
+        w.values(pf, st0, 1, lane);
+        if constexpr (more.value) w.raise(W::row_max(s0), c);
+      }
+    };
+    if (active) {
+      w.scores(s0, st0, 0, lane);
+      hide(s0, x, 0, ok0);
+      w.raise(W::row_max(s0), c);
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < W::RING; ++i) fr[i] = W::k_frag(st0, 1, i, lane);
+      }
+    }
+    for (; x + 1 < last; ++x) {
+      if (active) both(yes);
+      if (x + 2 < last) {
+        put(x + 2, st2, ok2);
+        if (x + 3 < last) ask();
       }
       __syncthreads();
+      char* st = st0;
+      st0 = st1; st1 = st2; st2 = st;
+      ok0 = ok1; ok1 = ok2;
     }
+    if (active) both(no);
+    __syncthreads();  // the last stage is no longer read
+    if (s_bad[item++ & 1] && active) w.template add_bad<F8>(kv, x0, last, first_pos, lane);
     const PagedAttnArgs& a = args_here();
     const float l = half_sum(w.l);
     const int hh = lane >> 5, l32 = lane & 31;
@@ -818,9 +1195,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int m_
 }
 
 template <typename T, int D, bool F8>
-static hipError_t attend_dispatch(const PagedAttnArgs& a, bool few, hipStream_t s) {
-  const int m_rows = few ? kPagedFewRows : kPagedTileRows, n_wg = paged_workgroups(few);
-  if (few) hipLaunchKernelGGL((paged_few_kernel<T, D, F8>), dim3(n_wg), dim3(256), 0, s, a);
+static hipError_t attend_dispatch(const PagedAttnArgs& a, PagedForm form, hipStream_t s) {
+  const int m_rows = paged_rows(form), n_wg = paged_workgroups(form);
+  if (form == PagedForm::kFew16) hipLaunchKernelGGL((paged_few_kernel<T, D, F8, 1>), dim3(n_wg), dim3(256), 0, s, a);
+  else if (form == PagedForm::kFew32) hipLaunchKernelGGL((paged_few_kernel<T, D, F8, 2>), dim3(n_wg), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((paged_tile_kernel<T, D, F8>), dim3(n_wg), dim3(512), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -829,12 +1207,12 @@ static hipError_t attend_dispatch(const PagedAttnArgs& a, bool few, hipStream_t 
   return hipGetLastError();
 }
 
-hipError_t launch_attend_paged(const PagedAttnArgs& a, bool few, bool e4m3, bool bf16, int head_dim, hipStream_t s) {
+hipError_t launch_attend_paged(const PagedAttnArgs& a, PagedForm form, bool e4m3, bool bf16, int head_dim, hipStream_t s) {
   if (bf16 && head_dim == 128)
-    return e4m3 ? attend_dispatch<__bf16, 128, true>(a, few, s) : attend_dispatch<__bf16, 128, false>(a, few, s);
+    return e4m3 ? attend_dispatch<__bf16, 128, true>(a, form, s) : attend_dispatch<__bf16, 128, false>(a, form, s);
   if (bf16)
-    return e4m3 ? attend_dispatch<__bf16, 64, true>(a, few, s) : attend_dispatch<__bf16, 64, false>(a, few, s);
-  return e4m3 ? attend_dispatch<float, 64, true>(a, few, s) : attend_dispatch<float, 64, false>(a, few, s);  // float32: head_dim 64
+    return e4m3 ? attend_dispatch<__bf16, 64, true>(a, form, s) : attend_dispatch<__bf16, 64, false>(a, form, s);
+  return e4m3 ? attend_dispatch<float, 64, true>(a, form, s) : attend_dispatch<float, 64, false>(a, form, s);  // float32: head_dim 64
 }
 
 }  // namespace hga
