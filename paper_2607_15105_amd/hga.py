@@ -145,9 +145,10 @@ def _ptr(t: torch.Tensor | None) -> int | None:
 
 
 def _strides(t: torch.Tensor) -> Strides:
-    if t.dim() != 3 or t.stride(2) != 1:
+    s = t.stride()
+    if len(s) != 3 or s[2] != 1:
         raise ValueError("expected a [rows, heads, head_dim] tensor with contiguous head_dim")
-    return Strides(t.stride(0), t.stride(1))
+    return Strides(s[0], s[1])
 
 
 def _stream() -> int:
@@ -463,6 +464,13 @@ class PagedCache:
     v_scale: torch.Tensor | None
     desc: PagedCacheDesc
 
+    def __post_init__(self):
+        self.ref = ctypes.byref(self.desc)
+        self.device = self.k.device
+        self.dtype = self.k.dtype
+        self.heads, self.head_dim = self.k.shape[2:]
+        self.n_seqs = self.desc.n_seqs
+
 
 def _need(ok: bool, what: str) -> None:
     if not ok:
@@ -513,44 +521,55 @@ def alloc_paged_cache(cfg: Config, n_seqs: int, table_cap: int, n_pages: int, pa
 
 
 def _check_batch(cfg: Config, cache: PagedCache, seq_rows: torch.Tensor, q_begin: torch.Tensor, heads: int,
-                 *rows: torch.Tensor) -> None:
-    """The arguments of a call over a ragged batch: what the kernels would
-    otherwise read out of bounds, and the device that they run on."""
-    n_seqs = cache.desc.n_seqs
-    _need(seq_rows.dtype == q_begin.dtype == torch.int32 and seq_rows.is_contiguous() and q_begin.is_contiguous()
-          and tuple(seq_rows.shape) == (n_seqs + 1,) and tuple(q_begin.shape) == (n_seqs,),
-          "seq_rows [n_seqs + 1], q_begin [n_seqs]: dense int32 tensors")
-    shape, dt = (rows[0].shape[0], heads, cfg.head_dim), _torch_dtype(cfg)
-    for t in rows:
-        _need(tuple(t.shape) == shape and t.dtype == dt, f"rows: [n_rows, {heads}, {cfg.head_dim}] tensors of {dt}")
-    dev = cache.k.device
-    _need(all(t.device == dev for t in (seq_rows, q_begin, *rows)), "all tensors lie on the cache's device")
-    _on_current(dev)
+                 a: torch.Tensor, b: torch.Tensor) -> int:
+    """The arguments of a call over a ragged batch (rows a and b): what the
+    kernels would otherwise read out of bounds. Returns the stream."""
+    n_seqs, dev = cache.n_seqs, cache.device
+    if not (seq_rows.dtype == q_begin.dtype == torch.int32 and seq_rows.is_contiguous() and q_begin.is_contiguous()
+            and seq_rows.shape == (n_seqs + 1,) and q_begin.shape == (n_seqs,)):
+        raise ValueError("seq_rows [n_seqs + 1], q_begin [n_seqs]: dense int32 tensors")
+    dt = _torch_dtype(cfg)
+    if not (a.shape[1:] == (heads, cfg.head_dim) and a.shape == b.shape and a.dtype == b.dtype == dt):
+        raise ValueError(f"rows: [n_rows, {heads}, {cfg.head_dim}] tensors of {dt}")
+    if cache.heads != cfg.n_kv_heads or cache.head_dim != cfg.head_dim or (cache.dtype != dt and cache.k_scale is None):
+        raise ValueError("the cache belongs to another configuration")
+    if not (seq_rows.device == dev and q_begin.device == dev and a.device == dev and b.device == dev):
+        raise ValueError("all tensors lie on the cache's device")
+    return _stream_on(dev)
 
 
-def _on_current(dev: torch.device) -> None:
-    _need(dev.type == "cuda", "expected GPU tensors")
-    _need(dev.index == torch.cuda.current_device(), "the tensors' device is not the current one")
+def _stream_on(dev: torch.device) -> int:
+    """The current stream, which has to be one of the tensors' device."""
+    if dev.type != "cuda":
+        raise ValueError("expected GPU tensors")
+    if torch.cuda.current_device() != dev.index:
+        raise ValueError("the tensors' device is not the current one")
+    return _raw_stream(dev.index)
+
+
+# The handle alone: torch.cuda.current_stream() builds a Stream around it, 2.8 us a call.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                      lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def cache_write(cfg: Config, cache: PagedCache, K: torch.Tensor, V: torch.Tensor, seq_rows: torch.Tensor,
                 q_begin: torch.Tensor) -> None:
     """Rows seq_rows[s] .. seq_rows[s + 1] - 1 of K, V [n_rows, Hkv, d] into
     positions q_begin[s] ... of sequence s, in the cache's format."""
-    _check_batch(cfg, cache, seq_rows, q_begin, cfg.n_kv_heads, K, V)
+    stream = _check_batch(cfg, cache, seq_rows, q_begin, cfg.n_kv_heads, K, V)
     _call("hga_cache_write",
-        ctypes.byref(cfg), ctypes.byref(cache.desc), _ptr(K), _strides(K), _ptr(V), _strides(V), K.shape[0],
-        _ptr(seq_rows), _ptr(q_begin), _stream())
+        ctypes.byref(cfg), cache.ref, K.data_ptr(), _strides(K), V.data_ptr(), _strides(V), K.shape[0],
+        seq_rows.data_ptr(), q_begin.data_ptr(), stream)
 
 
 def cache_read(cfg: Config, cache: PagedCache, K: torch.Tensor, V: torch.Tensor, seq_rows: torch.Tensor,
                q_begin: torch.Tensor) -> None:
     """The cached rows of those positions into K, V [n_rows, Hkv, d]; zeros
     where the page is absent."""
-    _check_batch(cfg, cache, seq_rows, q_begin, cfg.n_kv_heads, K, V)
+    stream = _check_batch(cfg, cache, seq_rows, q_begin, cfg.n_kv_heads, K, V)
     _call("hga_cache_read",
-        ctypes.byref(cfg), ctypes.byref(cache.desc), _ptr(K), _strides(K), _ptr(V), _strides(V), K.shape[0],
-        _ptr(seq_rows), _ptr(q_begin), _stream())
+        ctypes.byref(cfg), cache.ref, K.data_ptr(), _strides(K), V.data_ptr(), _strides(V), K.shape[0],
+        seq_rows.data_ptr(), q_begin.data_ptr(), stream)
 
 
 def gather_paged(cfg: Config, cache: PagedCache, seq: int, q_begin: int, n_q: int, sel_groups: torch.Tensor,
@@ -564,12 +583,13 @@ def gather_paged(cfg: Config, cache: PagedCache, seq: int, q_begin: int, n_q: in
           and n_sel_groups.numel() == Kc.shape[0] * Kc.shape[1]
           and sel_groups.numel() == n_sel_groups.numel() * max(cfg.top_groups, 1),
           "sel_groups [n_q/B, Hkv, top_groups], n_sel_groups [n_q/B, Hkv]: dense int32 tensors")
-    dev = cache.k.device
+    _need(cache.heads == cfg.n_kv_heads and cache.head_dim == cfg.head_dim
+          and (cache.k_scale is not None or cache.dtype == _torch_dtype(cfg)), "the cache belongs to another configuration")
+    dev = cache.device
     _need(all(t.device == dev for t in (sel_groups, n_sel_groups, Kc, Vc)), "all tensors lie on the cache's device")
-    _on_current(dev)
     _call("hga_gather_paged",
-        ctypes.byref(cfg), ctypes.byref(cache.desc), seq, q_begin, n_q, _ptr(sel_groups), _ptr(n_sel_groups), _ptr(Kc),
-        _ptr(Vc), Kc.shape[2], _stream())
+        ctypes.byref(cfg), cache.ref, seq, q_begin, n_q, _ptr(sel_groups), _ptr(n_sel_groups), _ptr(Kc),
+        _ptr(Vc), Kc.shape[2], _stream_on(dev))
 
 
 def paged_workspace_size(cfg: Config, n_rows: int, max_rows: int | None = None) -> int:
@@ -581,14 +601,15 @@ def attend_paged_fwd(cfg: Config, cache: PagedCache, Q: torch.Tensor, seq_rows: 
     """Dense causal attention of the rows of Q [n_rows, Hq, d] over their
     sequences' cached positions up to their own. max_rows: the most rows that a
     sequence of the call has (default: n_rows)."""
-    _check_batch(cfg, cache, seq_rows, q_begin, cfg.n_q_heads, Q, O)
-    _need(tuple(lse.shape) == (Q.shape[0], cfg.n_q_heads) and lse.dtype == torch.float32 and lse.is_contiguous()
-          and lse.device == Q.device == workspace.device,
-          "lse: a dense float32 [n_rows, Hq] tensor on the cache's device, as the workspace")
+    stream = _check_batch(cfg, cache, seq_rows, q_begin, cfg.n_q_heads, Q, O)
+    n_rows = Q.shape[0]
+    if not (lse.shape == (n_rows, cfg.n_q_heads) and lse.dtype == torch.float32 and lse.is_contiguous()
+            and lse.device == workspace.device == cache.device and workspace.is_contiguous()):
+        raise ValueError("lse: a dense float32 [n_rows, Hq] tensor on the cache's device, as the workspace")
     _call("hga_attend_paged_fwd",
-        ctypes.byref(cfg), ctypes.byref(cache.desc), _ptr(Q), _strides(Q), Q.shape[0], _ptr(seq_rows), _ptr(q_begin),
-        Q.shape[0] if max_rows is None else max_rows, _ptr(O), _strides(O), _ptr(lse), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream())
+        ctypes.byref(cfg), cache.ref, Q.data_ptr(), _strides(Q), n_rows, seq_rows.data_ptr(), q_begin.data_ptr(),
+        n_rows if max_rows is None else max_rows, O.data_ptr(), _strides(O), lse.data_ptr(), workspace.data_ptr(),
+        workspace.nbytes, stream)
 
 
 # ---------------------------------------------------------------------------
