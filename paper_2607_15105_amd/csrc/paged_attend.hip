@@ -981,12 +981,15 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
   using W = WaveRows<T, D, KT>;
   using Frag = typename W::Frag;
   constexpr int SB = W::ST::kBytes;
+  // the least share, in units: what a unit takes (bf16 2 us, float32 7) against a
+  // partial result's writing and joining
+  constexpr int kLeast = sizeof(T) == 2 ? 4 : 1;
   __shared__ __attribute__((aligned(16))) char smem[3 * SB];
   __shared__ int64_t s_scan[NW + 2];
   __shared__ int s_bad[2];  // whether V had what is not finite in this item, and in the next
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int shift = kPagedTileRowsLog2 - args_here().gqa_shift, wg = share_index();
-  const Share<kPagedTileKeys> share = take_share<512, kPagedTileWorkgroups, kPagedTileKeys>(wg, shift, 1, 4, s_scan);
+  const Share<kPagedTileKeys> share = take_share<512, kPagedTileWorkgroups, kPagedTileKeys>(wg, shift, 1, kLeast, s_scan);
   const float c = args_here().scale_log2;
   if (tid < 2) s_bad[tid] = 0;
   __syncthreads();
@@ -1093,38 +1096,66 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
     if (active) both(no);
     __syncthreads();  // the last stage is no longer read
     if (s_bad[item++ & 1] && active) w.template add_bad<F8>(kv, x0, last, first_pos, lane);
+    // A lane holds half the head dim of one row, so stores from registers would
+    // scatter over 32 rows each; the wave's rows go through its share of the
+    // stages instead and leave with consecutive lanes on consecutive pieces.
     const PagedAttnArgs& a = args_here();
     const float l = half_sum(w.l);
     const int hh = lane >> 5, l32 = lane & 31;
-    const int64_t f = f0 + l32;
-    if (f < nf) {
-      if (whole) {
-        float* lse;
-        char* dst = out_row(a, q.first, sh.h, f, lse);
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        if (hh == 0) *lse = lse_of(w.m, l, c);
+    constexpr int EB = W::EB, SHARE = 3 * SB / NW / 16 * 16, OP = D * EB + 16, HP = D / 2 * 4 + 16;
+    static_assert(32 * OP <= SHARE && 32 * HP <= SHARE, "a wave's rows fit its share");
+    char* ost = smem + wave * SHARE;
+    const int rows = nf - f0 < 32 ? (int)(nf - f0) : 32;  // of the wave; none if not active
+    if (whole) {
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-        for (int dt = 0; dt < W::NDT; ++dt)
+      for (int dt = 0; dt < W::NDT; ++dt)
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4)
+          store4(ost + l32 * OP + (32 * dt + 8 * v4 + 4 * hh) * EB,
+                 f32x4{w.oacc[dt][4 * v4], w.oacc[dt][4 * v4 + 1], w.oacc[dt][4 * v4 + 2], w.oacc[dt][4 * v4 + 3]} * inv,
+                 EB == 2);
+      float* lse;
+      if (l32 < rows && hh == 0) {
+        out_row(a, q.first, sh.h, f0 + l32, lse);
+        *lse = lse_of(w.m, l, c);
+      }
+      __builtin_amdgcn_wave_barrier();
+      constexpr int CPR = D * EB / 16;
+#pragma unroll
+      for (int i = 0; i < 32 * CPR / 64; ++i) {
+        const int r = (lane + 64 * i) / CPR, p = (lane + 64 * i) % CPR;
+        if (r < rows)
+          *reinterpret_cast<u32x4*>(out_row(a, q.first, sh.h, f0 + r, lse) + p * 16) =
+              *reinterpret_cast<const u32x4*>(ost + r * OP + p * 16);
+      }
+    } else {
+      const int64_t at = ((int64_t)wg * 2 + (sh.kt == 0 ? 1 : 0)) * a.slot_rows + 32 * wave;
+      if (l32 < rows && hh == 0) {
+        a.part_ml[(at + l32) * 2] = w.m;
+        a.part_ml[(at + l32) * 2 + 1] = l;
+      }
+      constexpr int HD = W::NDT / 2, CPR = D / 2 * 4 / 16;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {  // float32 rows: half the head dim at a time
+#pragma unroll
+        for (int dt = half * HD; dt < (half + 1) * HD; ++dt)
 #pragma unroll
           for (int v4 = 0; v4 < 4; ++v4)
-            store4(dst + (32 * dt + 8 * v4 + 4 * hh) * W::EB,
-                   f32x4{w.oacc[dt][4 * v4], w.oacc[dt][4 * v4 + 1], w.oacc[dt][4 * v4 + 2], w.oacc[dt][4 * v4 + 3]} * inv,
-                   W::EB == 2);
-      } else {
-        const int64_t at = ((int64_t)wg * 2 + (sh.kt == 0 ? 1 : 0)) * a.slot_rows + 32 * wave + l32;
-        float* dst = a.part + at * D;
-#pragma unroll
-        for (int dt = 0; dt < W::NDT; ++dt)
-#pragma unroll
-          for (int v4 = 0; v4 < 4; ++v4)
-            *reinterpret_cast<f32x4*>(dst + 32 * dt + 8 * v4 + 4 * hh) =
+            *reinterpret_cast<f32x4*>(ost + l32 * HP + (32 * (dt - half * HD) + 8 * v4 + 4 * hh) * 4) =
                 f32x4{w.oacc[dt][4 * v4], w.oacc[dt][4 * v4 + 1], w.oacc[dt][4 * v4 + 2], w.oacc[dt][4 * v4 + 3]};
-        if (hh == 0) {
-          a.part_ml[at * 2] = w.m;
-          a.part_ml[at * 2 + 1] = l;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 32 * CPR / 64; ++i) {
+          const int r = (lane + 64 * i) / CPR, p = (lane + 64 * i) % CPR;
+          if (r < rows)
+            *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(a.part + (at + r) * D + half * (D / 2)) + p * 16) =
+                *reinterpret_cast<const u32x4*>(ost + r * HP + p * 16);
         }
+        __builtin_amdgcn_wave_barrier();
       }
     }
+    __syncthreads();  // the stages are free again
   });
 }
 
