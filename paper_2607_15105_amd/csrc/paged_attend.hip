@@ -446,6 +446,10 @@ __device__ inline const char* query_row(const PagedAttnArgs& a, int first, int h
   return row_ptr(a.Q, first + (f >> a.gqa_shift), a.q_tok) + hq * a.q_head;
 }
 
+// How far, in raw scores, a row's maximum may lie above the one in use: 2^8 in
+// p. Finite for any scale, so that a score is above -inf plus it.
+__device__ inline float slack(float c) { return fminf(8.0f / c, 3.0e38f); }
+
 // ---------------------------------------------------------------- one wave's rows
 
 // 32 folded rows of one wave, over KT-key tiles: lane l holds (half the head
@@ -509,7 +513,7 @@ struct WaveRows {
   }
   // The running maximum follows mx, O and the sum with it, where it grew by over 2^8.
   __device__ __forceinline__ void raise(float mx, float c) {
-    const bool up = mx > m + 8.0f / c;  // the first finite score too: m = -inf
+    const bool up = mx > m + slack(c);  // the first finite score too: m = -inf
     if (__any(up)) {
       const float mn = up ? mx : m;
       const float corr = up ? __builtin_amdgcn_exp2f((m - mn) * c) : 1.0f;
@@ -776,7 +780,7 @@ struct FewRows {
       float other = mx;
       swap16(mx, other);
       mx = half_max(fmaxf(mx, other));
-      const bool up = mx > m[r] + 8.0f / c;  // the first finite score too: m = -inf
+      const bool up = mx > m[r] + slack(c);  // the first finite score too: m = -inf
       if (__any(up)) {
         const float mn = up ? mx : m[r];
         const float corr = up ? __builtin_amdgcn_exp2f((m[r] - mn) * c) : 1.0f;

@@ -208,9 +208,10 @@ def test_rows_of_many_sequences_find_their_place():
 
 # ---------------------------------------------------------------- attention
 
-def _attend_check(cfg, cache, Q, first, begin, Kd, Vd, max_rows=None, O=None, what=""):
+def _attend_check(cfg, cache, Q, first, begin, Kd, Vd, max_rows=None, O=None, what="", only=None):
     """attend_paged_fwd against float64; Kd, Vd: per sequence the held rows of
-    positions 0 .. [L, Hkv, d] in float64. Returns (O, lse)."""
+    positions 0 .. [L, Hkv, d] in float64; `only`: the sequences that are compared
+    (all). Returns (O, lse)."""
     n = Q.shape[0]
     O = torch.full_like(Q, 7.0) if O is None else O
     lse = torch.full((n, cfg.n_q_heads), 7.0, device="cuda")
@@ -228,6 +229,8 @@ def _attend_check(cfg, cache, Q, first, begin, Kd, Vd, max_rows=None, O=None, wh
         if b <= a:
             continue
         mine[a:b] = True
+        if only is not None and s not in only:
+            continue
         L = Kd[s].shape[0]
         t = torch.arange(L)
         at = t // page
@@ -436,7 +439,103 @@ def test_two_sequences_share_a_prefix():
     _attend_check(cfg, cache, Q, [0, 1, 21], [89, 28], [Kd[0], Kd[0][:48]], [Vd[0], Vd[0][:48]], 20, what="shared")
 
 
+@pytest.mark.parametrize("rows,e4m3", [(1, False), (1, True), (3, False), (3, True)])
+def test_long_shares(rows, e4m3):
+    """64 sequences over the same 20,000 cached positions: enough work that a
+    workgroup follows one context over hundreds of tiles."""
+    say(f"[attend] long shares, {rows} rows, e4m3 {e4m3}")
+    gen = torch.Generator().manual_seed(22)
+    cfg = _cfg(64, 8, 64, BF)
+    ctx, S = 20000, 64
+    cache = _cache(cfg, S, 160, 161, 128, e4m3, "head", fill=0xFF)
+    _fill_table(cache, [ctx] + [0] * (S - 1), gen)
+    Kd, Vd = _context(cfg, cache, [ctx] + [0] * (S - 1), gen, e4m3)
+    cache.page_table[1:] = cache.page_table[0]
+    cache.page_table[40, 70] = -1
+    Q = torch.randn(rows * S, 64, 64, generator=gen).to(BF).cuda()
+    begin = [ctx - rows - 37 * s for s in range(S)]
+    _attend_check(cfg, cache, Q, [rows * s for s in range(S + 1)], begin, [Kd[0]] * S, [Vd[0]] * S, rows, only=(0, 7, 40, 63))
+
+
+@pytest.mark.parametrize("max_rows", [1, 3, 9, None])
+def test_more_sequences_than_threads(max_rows):
+    gen = torch.Generator().manual_seed(23)
+    cfg = _cfg(4, 2, 64, BF)
+    S = 1100
+    rows = [int(x) for x in torch.randint(0, 3, (S,), generator=gen)]
+    rows[700], rows[1099] = 9, 9
+    ctx = [r + int(x) if r else 0 for r, x in zip(rows, torch.randint(0, 40, (S,), generator=gen))]
+    cache = _cache(cfg, S, 4, sum(-(-c // 16) for c in ctx) + 1, 16, False, "token", fill=0xFF)
+    _fill_table(cache, ctx, gen)
+    Kd, Vd = _context(cfg, cache, ctx, gen, False)
+    first = [0]
+    for r in rows:
+        first.append(first[-1] + r)
+    Q = torch.randn(first[-1], 4, 64, generator=gen).to(BF).cuda()
+    _attend_check(cfg, cache, Q, first, [c - r for c, r in zip(ctx, rows)], Kd, Vd, max_rows, what=f"{S} sequences")
+
+
+def test_a_tiny_scale_and_equal_keys():
+    """Every p alike: O is the mean of the values, lse the logarithm of their number."""
+    gen = torch.Generator().manual_seed(24)
+    cfg = _cfg(4, 2, 128, BF, softmax_scale=1e-38)
+    cache = _cache(cfg, 1, 10, 10, 16, False, "head", fill=0xFF)
+    _fill_table(cache, [150], gen)
+    Kd, Vd = _context(cfg, cache, [150], gen, False)
+    Q = torch.randn(40, 4, 128, generator=gen).to(BF).cuda()
+    for max_rows in (1, 40):
+        _attend_check(cfg, cache, Q, [0, 40], [110], Kd, Vd, max_rows)
+
+
 # ---------------------------------------------------------------- streams, graphs
+
+def test_recorded_calls_and_graphs_that_share_a_workspace():
+    """Calls marshalled once, and two captured graphs with one workspace replayed
+    one after the other: the direct calls' bits."""
+    gen = torch.Generator().manual_seed(25)
+    cfg = _cfg(8, 2, 128, BF)
+    cache = _cache(cfg, 2, 30, 60, 64, True, "head")
+    _fill_table(cache, [1900, 900], gen)
+    K, V = (torch.randn(2800, 2, 128, generator=gen).to(BF).cuda() for _ in range(2))
+    calls = []
+    ws = torch.empty(hga.paged_workspace_size(cfg, 300, 200), dtype=torch.uint8, device="cuda")
+    for rows in ([1, 1], [200, 100]):
+        Q = torch.randn(sum(rows), 8, 128, generator=gen).to(BF).cuda()
+        first, begin = _rows([0, rows[0], sum(rows)]), _rows([1900 - rows[0], 900 - rows[1]])
+        calls.append((Q, first, begin, torch.zeros_like(Q), torch.zeros(sum(rows), 8, device="cuda"), max(rows)))
+
+    def attend(i):
+        Q, first, begin, O, lse, most = calls[i]
+        hga.attend_paged_fwd(cfg, cache, Q, first, begin, O, lse, ws, most)
+
+    first, begin = _rows([0, 1900, 2800]), _rows([0, 0])  # kept: the recorded call has their addresses
+    with hga.record() as kept:
+        hga.cache_write(cfg, cache, K, V, first, begin)
+        attend(0)
+        attend(1)
+    assert not bool(cache.k.float().any())  # recorded, not made
+    for call in kept:
+        call()
+    torch.cuda.synchronize()
+    want = [(c[3].clone(), c[4].clone()) for c in calls]
+    assert all(bool(w[0].float().abs().sum() > 0) for w in want)
+    side, graphs = torch.cuda.Stream(), [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for i in range(2):
+        with torch.cuda.graph(graphs[i], stream=side):
+            attend(i)
+    for turn in range(4):
+        for c in calls:
+            c[3].zero_()
+            c[4].zero_()
+        ws.fill_(255)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graphs[turn % 2].replay()
+            graphs[1 - turn % 2].replay()
+        side.synchronize()
+        for c, (o, z) in zip(calls, want):
+            assert torch.equal(c[3], o) and torch.equal(c[4], z)
+
 
 def test_captured_steps_follow_the_lengths_on_the_device():
     """One decode step (write, attend) captured once and replayed as the
