@@ -772,7 +772,7 @@ struct FewRows {
             if (!((see >> (16 * t + v)) & 1)) s[r][t][v] = -__builtin_inff();
       }
     }
-    Frag pf[NR];
+    Frag pf[NR], plo[NR];  // bf16: P as a pair hi + lo, to about 2^-17, as in the per-query forward
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       float mx = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])),
@@ -799,9 +799,13 @@ struct FewRows {
           sum += s[r][t][v];
         }
       l[r] += sum;
-      if constexpr (EB == 2)  // P is rounded to the inputs' precision, as in the routed forward
+      if constexpr (EB == 2)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) pf[r][j] = (__bf16)s[r][j >> 2][j & 3];
+        for (int j = 0; j < 8; ++j) {
+          const float p = s[r][j >> 2][j & 3];
+          pf[r][j] = (__bf16)p;
+          plo[r][j] = (__bf16)(p - (float)pf[r][j]);
+        }
     }
     if constexpr (EB == 2) {
 #pragma unroll
@@ -813,7 +817,7 @@ struct FewRows {
         const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(p + 16 * ST::kVPitch));
         const Frag vf = __builtin_bit_cast(Frag, (s16x8)__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-        for (int r = 0; r < NR; ++r) oacc[r][dt] = EL::mma(vf, pf[r], oacc[r][dt]);
+        for (int r = 0; r < NR; ++r) oacc[r][dt] = EL::mma(vf, plo[r], EL::mma(vf, pf[r], oacc[r][dt]));
       }
     } else {
 #pragma unroll
