@@ -910,9 +910,9 @@ static int slot_rows(const hga_config_t* c, int64_t n_rows, PagedForm form) {
 }
 static size_t paged_ws(const hga_config_t* c, int64_t n_rows, PagedForm form) {
   const size_t rows = 2 * (size_t)hga::paged_workgroups(form) * slot_rows(c, n_rows, form);
-  return hga::paged_workgroups(form) * sizeof(int4) + rows * (c->head_dim + 2) * sizeof(float);
+  return hga::paged_workgroups(form) * sizeof(int4) + rows * (c->head_dim + 2) * sizeof(float);  // a multiple of 16
 }
-// The forms a call runs, one after the other: of few rows only where no sequence is
+// The forms a call runs: of few rows only where no sequence is
 // expected to have more than that form takes at a time; else the form of many
 // rows, and for the sequences of few rows beside them (generation beside a
 // prompt's chunk) that of 16. A form of its own takes whatever there is.
@@ -930,12 +930,9 @@ static int paged_forms(const hga_config_t* c, int64_t n_seqs, int64_t max_rows, 
 size_t hga_paged_workspace_size(const hga_config_t* cfg, int64_t n_rows, int64_t max_rows) {
   if (check_cfg(cfg) != HGA_OK || n_rows < 1 || n_rows >= kMaxTokens || max_rows < 1) return 0;
   PagedForm forms[2];
-  size_t most = 0;
-  for (int i = 0, n = paged_forms(cfg, 2, max_rows, forms); i < n; ++i) {
-    const size_t need = paged_ws(cfg, n_rows, forms[i]);
-    if (need > most) most = need;
-  }
-  return most;
+  size_t need = 0;
+  for (int i = 0, n = paged_forms(cfg, 2, max_rows, forms); i < n; ++i) need += paged_ws(cfg, n_rows, forms[i]);
+  return need;
 }
 
 hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache_t* cache, const void* Q,
@@ -958,21 +955,24 @@ hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache
   a.lse = lse;
   a.n_q_heads = cfg->n_q_heads; a.gqa_shift = log2_exact(G);
   a.scale_log2 = eff_scale(cfg) * 1.4426950408889634f;
-  a.info = static_cast<int4*>(workspace);
-  const bool e4m3 = cache->format == HGA_CACHE_E4M3, bf16 = cfg->dtype == HGA_BF16;
   PagedForm forms[2];
-  const int n_forms = paged_forms(cfg, cache->n_seqs, max_rows, forms);
-  for (int i = 0; i < n_forms; ++i) {  // they share the workspace
-    const PagedForm form = forms[i];
-    const int few_rows = 16 / G;
-    a.min_rows = n_forms == 2 && form == PagedForm::kTile ? few_rows + 1 : 1;
-    a.max_rows = n_forms == 2 && form != PagedForm::kTile ? few_rows : 0x7fffffff;
-    a.slot_rows = slot_rows(cfg, n_rows, form);
-    a.part = reinterpret_cast<float*>(a.info + hga::paged_workgroups(form));
-    a.part_ml = a.part + 2 * (int64_t)hga::paged_workgroups(form) * a.slot_rows * cfg->head_dim;
-    if (hga::launch_attend_paged(a, form, e4m3, bf16, cfg->head_dim, (hipStream_t)stream) != hipSuccess)
-      return HGA_ERR_HIP;
+  hga::PagedAttnArgs args[2];
+  const int n_forms = paged_forms(cfg, cache->n_seqs, max_rows, forms), few_rows = 16 / G;
+  char* ws = static_cast<char*>(workspace);
+  for (int i = 0; i < n_forms; ++i) {
+    const bool tile = forms[i] == PagedForm::kTile;
+    a.min_rows = n_forms == 2 && tile ? few_rows + 1 : 1;
+    a.max_rows = n_forms == 2 && !tile ? few_rows : 0x7fffffff;
+    a.slot_rows = slot_rows(cfg, n_rows, forms[i]);
+    a.info = reinterpret_cast<int4*>(ws);
+    a.part = reinterpret_cast<float*>(a.info + hga::paged_workgroups(forms[i]));
+    a.part_ml = a.part + 2 * (int64_t)hga::paged_workgroups(forms[i]) * a.slot_rows * cfg->head_dim;
+    ws += paged_ws(cfg, n_rows, forms[i]);
+    args[i] = a;
   }
+  if (hga::launch_attend_paged(args, forms, n_forms, cache->format == HGA_CACHE_E4M3, cfg->dtype == HGA_BF16,
+                               cfg->head_dim, (hipStream_t)stream) != hipSuccess)
+    return HGA_ERR_HIP;
   return HGA_OK;
 }
 

@@ -1174,10 +1174,13 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
 // sums at once and hand the weights round, and the parts' rows are read eight
 // at a time. What bounds it is that chain of four round trips.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int m_rows) {
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs one, int one_rows, int n_one, PagedAttnArgs two,
+                                                         int two_rows) {
   constexpr int EB = Elem<T>::kBytes, V = D / 32;
   typedef float fV __attribute__((ext_vector_type(V)));
-  const int wg = blockIdx.x;
+  const bool first = (int)blockIdx.x < n_one;  // the workgroups of the first form, then the second's
+  const PagedAttnArgs& a = first ? one : two;
+  const int wg = first ? blockIdx.x : blockIdx.x - n_one, m_rows = first ? one_rows : two_rows;
   const int4 rec = a.info[wg];
   if (rec.x == 0) return;
   const SeqShape<6> q = shape_of<6>(a, rec.y, 0);
@@ -1234,24 +1237,32 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int m_
 }
 
 template <typename T, int D, bool F8>
-static hipError_t attend_dispatch(const PagedAttnArgs& a, PagedForm form, hipStream_t s) {
-  const int m_rows = paged_rows(form), n_wg = paged_workgroups(form);
-  if (form == PagedForm::kFew16) hipLaunchKernelGGL((paged_few_kernel<T, D, F8, 1>), dim3(n_wg), dim3(256), 0, s, a);
-  else if (form == PagedForm::kFew32) hipLaunchKernelGGL((paged_few_kernel<T, D, F8, 2>), dim3(n_wg), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((paged_tile_kernel<T, D, F8>), dim3(n_wg), dim3(512), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int rows = a.slot_rows < m_rows ? a.slot_rows : m_rows;
-  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(n_wg, (rows + 7) / 8), dim3(256), 0, s, a, m_rows);
+static hipError_t attend_dispatch(const PagedAttnArgs* a, const PagedForm* form, int n, hipStream_t s) {
+  int rows = 0;
+  for (int i = 0; i < n; ++i) {
+    const dim3 grid(paged_workgroups(form[i]));
+    if (form[i] == PagedForm::kFew16) hipLaunchKernelGGL((paged_few_kernel<T, D, F8, 1>), grid, dim3(256), 0, s, a[i]);
+    else if (form[i] == PagedForm::kFew32) hipLaunchKernelGGL((paged_few_kernel<T, D, F8, 2>), grid, dim3(256), 0, s, a[i]);
+    else hipLaunchKernelGGL((paged_tile_kernel<T, D, F8>), grid, dim3(512), 0, s, a[i]);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int m = a[i].slot_rows < paged_rows(form[i]) ? a[i].slot_rows : paged_rows(form[i]);
+    if (m > rows) rows = m;
+  }
+  const int one = paged_workgroups(form[0]), two = n > 1 ? paged_workgroups(form[1]) : 0;
+  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(one + two, (rows + 7) / 8), dim3(256), 0, s, a[0],
+                     paged_rows(form[0]), one, a[n - 1], paged_rows(form[n - 1]));
   return hipGetLastError();
 }
 
-hipError_t launch_attend_paged(const PagedAttnArgs& a, PagedForm form, bool e4m3, bool bf16, int head_dim, hipStream_t s) {
+hipError_t launch_attend_paged(const PagedAttnArgs* a, const PagedForm* form, int n, bool e4m3, bool bf16, int head_dim,
+                               hipStream_t s) {
   if (bf16 && head_dim == 128)
-    return e4m3 ? attend_dispatch<__bf16, 128, true>(a, form, s) : attend_dispatch<__bf16, 128, false>(a, form, s);
+    return e4m3 ? attend_dispatch<__bf16, 128, true>(a, form, n, s) : attend_dispatch<__bf16, 128, false>(a, form, n, s);
   if (bf16)
-    return e4m3 ? attend_dispatch<__bf16, 64, true>(a, form, s) : attend_dispatch<__bf16, 64, false>(a, form, s);
-  return e4m3 ? attend_dispatch<float, 64, true>(a, form, s) : attend_dispatch<float, 64, false>(a, form, s);  // float32: head_dim 64
+    return e4m3 ? attend_dispatch<__bf16, 64, true>(a, form, n, s) : attend_dispatch<__bf16, 64, false>(a, form, n, s);
+  // float32: head_dim 64
+  return e4m3 ? attend_dispatch<float, 64, true>(a, form, n, s) : attend_dispatch<float, 64, false>(a, form, n, s);
 }
 
 }  // namespace hga
