@@ -1175,17 +1175,18 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
 // at a time. What bounds it is that chain of four round trips.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs one, int one_rows, int n_one, PagedAttnArgs two,
-                                                         int two_rows) {
+                                                         int two_rows) {  // n_one: workgroups for the first form's parts
   constexpr int EB = Elem<T>::kBytes, V = D / 32;
   typedef float fV __attribute__((ext_vector_type(V)));
-  const bool first = (int)blockIdx.x < n_one;  // the workgroups of the first form, then the second's
+  const bool first = (int)blockIdx.x < n_one;
   const PagedAttnArgs& a = first ? one : two;
-  const int wg = first ? blockIdx.x : blockIdx.x - n_one, m_rows = first ? one_rows : two_rows;
+  const int m_rows = first ? one_rows : two_rows, groups = ((a.slot_rows < m_rows ? a.slot_rows : m_rows) + 7) / 8;
+  const int id = first ? blockIdx.x : blockIdx.x - n_one, wg = id / groups;
   const int4 rec = a.info[wg];
   if (rec.x == 0) return;
   const SeqShape<6> q = shape_of<6>(a, rec.y, 0);
   const int64_t nf = (int64_t)q.n << a.gqa_shift, f0 = (int64_t)rec.w * m_rows;
-  const int row = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int row = id % groups * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (row >= m_rows || f0 + row >= nf) return;
   const float c = a.scale_log2;
   // part k is the share wg + k's: the first one its last item, the others their first
@@ -1238,7 +1239,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs one, int 
 
 template <typename T, int D, bool F8>
 static hipError_t attend_dispatch(const PagedAttnArgs* a, const PagedForm* form, int n, hipStream_t s) {
-  int rows = 0;
+  int join[2] = {0, 0};
   for (int i = 0; i < n; ++i) {
     const dim3 grid(paged_workgroups(form[i]));
     if (form[i] == PagedForm::kFew16) hipLaunchKernelGGL((paged_few_kernel<T, D, F8, 1>), grid, dim3(256), 0, s, a[i]);
@@ -1246,12 +1247,11 @@ static hipError_t attend_dispatch(const PagedAttnArgs* a, const PagedForm* form,
     else hipLaunchKernelGGL((paged_tile_kernel<T, D, F8>), grid, dim3(512), 0, s, a[i]);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int m = a[i].slot_rows < paged_rows(form[i]) ? a[i].slot_rows : paged_rows(form[i]);
-    if (m > rows) rows = m;
+    const int rows = a[i].slot_rows < paged_rows(form[i]) ? a[i].slot_rows : paged_rows(form[i]);
+    join[i] = paged_workgroups(form[i]) * ((rows + 7) / 8);
   }
-  const int one = paged_workgroups(form[0]), two = n > 1 ? paged_workgroups(form[1]) : 0;
-  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(one + two, (rows + 7) / 8), dim3(256), 0, s, a[0],
-                     paged_rows(form[0]), one, a[n - 1], paged_rows(form[n - 1]));
+  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(join[0] + join[1]), dim3(256), 0, s, a[0], paged_rows(form[0]),
+                     join[0], a[n - 1], paged_rows(form[n - 1]));
   return hipGetLastError();
 }
 
