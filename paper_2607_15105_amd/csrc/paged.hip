@@ -36,9 +36,7 @@ struct RowPlace {
   int seq, page, slot;
 };
 __device__ inline RowPlace place_of(const PagedArgs& a, int64_t r, int lane) {
-  int seq[1];
-  find_rows<1>(a, r, lane, seq);
-  RowPlace p = {__builtin_amdgcn_readfirstlane(seq[0]), -1, 0};
+  RowPlace p = {__builtin_amdgcn_readfirstlane(seq_of_row(a, r, lane)), -1, 0};
   if (p.seq >= 0) {
     const int64_t t = (int64_t)a.q_begin[p.seq] + (r - a.seq_rows[p.seq]);
     p.page = page_of(a, p.seq, t);
@@ -71,10 +69,10 @@ constexpr int kPasses = 2;  // head groups of a row whose pieces are under way a
 // rows of 8 heads, d = 128, bf16 to 8 bits took 10.7 us and 7,896 rows 16.1 us
 // with four rows to a wave, one after the other.
 template <typename T, int D, bool F8>
-__global__ __launch_bounds__(256) void cache_write_kernel(PagedArgs a, DenseRows d) {
+__global__ __launch_bounds__(256) void cache_write_kernel(PagedArgs a, DenseRows d, int64_t first) {
   constexpr int EB = Elem<T>::kBytes, LPR = D * EB / 16, HP = 64 / LPR, N = 16 / EB;
   const int lane = threadIdx.x & 63, c = lane % LPR;
-  const int64_t r = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t r = first + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (r >= a.n_rows) return;
   const RowPlace at = place_of(a, r, lane);
   if (at.page < 0) return;
@@ -121,10 +119,10 @@ __global__ __launch_bounds__(256) void cache_write_kernel(PagedArgs a, DenseRows
 
 // Rows out of the cache, one per wave; an absent page's rows are zeros.
 template <typename T, int D, bool F8>
-__global__ __launch_bounds__(256) void cache_read_kernel(PagedArgs a, DenseRows d) {
+__global__ __launch_bounds__(256) void cache_read_kernel(PagedArgs a, DenseRows d, int64_t first) {
   constexpr int EB = Elem<T>::kBytes, LPR = D * EB / 16, HP = 64 / LPR;
   const int lane = threadIdx.x & 63, c = lane % LPR;
-  const int64_t r = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t r = first + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (r >= a.n_rows) return;
   const RowPlace at = place_of(a, r, lane);
   if (at.seq < 0) return;
@@ -209,18 +207,26 @@ __global__ __launch_bounds__(256) void gather_paged_kernel(AttnArgs a, PagedArgs
     }                                                \
   } while (0)
 
+// Rows of a launch: a grid holds fewer than 2^32 threads, 64 to a row.
+constexpr int64_t kLaunchRows = 1 << 25;
+static unsigned row_workgroups(int64_t rows) { return (unsigned)(((rows < kLaunchRows ? rows : kLaunchRows) + 3) / 4); }
+
 hipError_t launch_cache_write(const PagedArgs& a, const DenseRows& d, bool e4m3, bool bf16, int head_dim, hipStream_t s) {
-  const dim3 grid((unsigned)((a.n_rows + 3) / 4));
-#define HGA_CALL(T, D, F) hipLaunchKernelGGL((cache_write_kernel<T, D, F>), grid, dim3(256), 0, s, a, d)
-  HGA_PAGED_DISPATCH(HGA_CALL);
+#define HGA_CALL(T, D, F) hipLaunchKernelGGL((cache_write_kernel<T, D, F>), grid, dim3(256), 0, s, a, d, first)
+  for (int64_t first = 0; first < a.n_rows; first += kLaunchRows) {
+    const dim3 grid(row_workgroups(a.n_rows - first));
+    HGA_PAGED_DISPATCH(HGA_CALL);
+  }
 #undef HGA_CALL
   return hipGetLastError();
 }
 
 hipError_t launch_cache_read(const PagedArgs& a, const DenseRows& d, bool e4m3, bool bf16, int head_dim, hipStream_t s) {
-  const dim3 grid((unsigned)((a.n_rows + 3) / 4));
-#define HGA_CALL(T, D, F) hipLaunchKernelGGL((cache_read_kernel<T, D, F>), grid, dim3(256), 0, s, a, d)
-  HGA_PAGED_DISPATCH(HGA_CALL);
+#define HGA_CALL(T, D, F) hipLaunchKernelGGL((cache_read_kernel<T, D, F>), grid, dim3(256), 0, s, a, d, first)
+  for (int64_t first = 0; first < a.n_rows; first += kLaunchRows) {
+    const dim3 grid(row_workgroups(a.n_rows - first));
+    HGA_PAGED_DISPATCH(HGA_CALL);
+  }
 #undef HGA_CALL
   return hipGetLastError();
 }

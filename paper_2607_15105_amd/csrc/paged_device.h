@@ -91,20 +91,16 @@ __device__ inline void rows_of(const PagedArgs& a, int s, int& first, int& n) {
   if (n < 0 || b < 0) n = 0;
 }
 
-// Sequence and position of the call's rows r0 + i, i < NR (the same r0 in the
-// whole wave): 64 entries of seq_rows at a time, counted by ballot, so that
-// any number of sequences costs independent loads and no search. seq[i] is -1
-// for a row of no sequence.
-template <int NR>
-__device__ inline void find_rows(const PagedArgs& a, int64_t r0, int lane, int (&seq)[NR]) {
-  int cnt[NR] = {};
+// Sequence of the call's row r (the same in the whole wave), -1 if it is of none:
+// 64 entries of seq_rows at a time, counted by ballot, so that any number of
+// sequences costs independent loads and no search.
+__device__ inline int seq_of_row(const PagedArgs& a, int64_t r, int lane) {
+  int cnt = 0;
   for (int base = 0; base <= a.n_seqs; base += 64) {
     const int v = base + lane <= a.n_seqs ? a.seq_rows[base + lane] : 0x7fffffff;
-#pragma unroll
-    for (int i = 0; i < NR; ++i) cnt[i] += __popcll(__ballot((int64_t)v <= r0 + i));
+    cnt += __popcll(__ballot((int64_t)v <= r));
   }
-#pragma unroll
-  for (int i = 0; i < NR; ++i) seq[i] = r0 + i < a.n_rows && cnt[i] >= 1 && cnt[i] <= a.n_seqs ? cnt[i] - 1 : -1;
+  return r < a.n_rows && cnt >= 1 && cnt <= a.n_seqs ? cnt - 1 : -1;
 }
 
 }  // namespace hga

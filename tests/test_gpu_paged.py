@@ -665,3 +665,82 @@ def test_routed_path_over_the_cache_equals_the_dense_rows(hq, hkv, d, dtype, e4m
     V[gone * page:gone * page + page] = 0
     hga.gather_routed(cfg, K, V, q0, n_q, rb.sel_groups, rb.n_sel_groups, a[0], a[1])
     assert torch.equal(a, b)
+
+
+# ---------------------------------------------------------------- the ends of the ranges
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("first", [[0, 0, 0], [40, 40, 40], [17, 17, 17]])
+def test_a_batch_without_rows_changes_nothing(first, e4m3):
+    cfg = _cfg(4, 2, 64, BF)
+    cache = _cache(cfg, 2, 4, 8, 16, e4m3, "head", fill=0x11)
+    cache.page_table.copy_(torch.arange(8).view(2, 4))
+    before = [t.view(torch.uint8).clone() for t in (cache.k, cache.v)]
+    x = torch.ones(40, 2, 64, dtype=BF, device="cuda")
+    rows, begin = _rows(first), _rows([3, 9])
+    hga.cache_write(cfg, cache, x, x, rows, begin)
+    assert all(torch.equal(t.view(torch.uint8), b) for t, b in zip((cache.k, cache.v), before))
+    out = torch.full((2, 40, 2, 64), 7.0, dtype=BF, device="cuda")
+    hga.cache_read(cfg, cache, out[0], out[1], rows, begin)
+    O, lse = torch.full((40, 4, 64), 7.0, dtype=BF, device="cuda"), torch.full((40, 4), 7.0, device="cuda")
+    for max_rows in (1, 16, 40):
+        ws = torch.full((hga.paged_workspace_size(cfg, 40, max_rows),), 255, dtype=torch.uint8, device="cuda")
+        hga.attend_paged_fwd(cfg, cache, O, rows, begin, O, lse, ws, max_rows)
+    assert bool((out == 7).all()) and bool((O == 7).all()) and bool((lse == 7).all())
+
+
+def test_more_rows_than_a_launch_has():
+    """2^26 rows and some, of which only the last belong to sequences."""
+    cfg = _cfg(1, 1, 64, BF)
+    n = (1 << 26) + 7
+    say(f"[write, read] {n} rows")
+    cache = _cache(cfg, 2, 2, 4, 16, False, "head")
+    cache.page_table.copy_(torch.arange(4).view(2, 2))
+    a, b = (torch.empty(n, 1, 64, dtype=BF, device="cuda") for _ in range(2))
+    gen = torch.Generator().manual_seed(31)
+    tail = torch.randn(8, 1, 64, generator=gen).to(BF).cuda()
+    a[n - 8:], b[n - 8:], a[:4], b[:4] = tail, -tail, 5.0, 5.0
+    first, begin = _rows([n - 5, n - 2, n]), _rows([0, 15])
+    hga.cache_write(cfg, cache, a, b, first, begin)
+    k, v = cache.k.cpu(), cache.v.cpu()
+    at = [(0, 0), (0, 1), (0, 2), (2, 15), (3, 0)]  # page, slot
+    want = torch.zeros_like(k)
+    for (p, t), row in zip(at, tail[3:].cpu()):
+        want[p, t] = row
+    assert torch.equal(k, want) and torch.equal(v, -want)
+    a[n - 8:], b[n - 8:] = 7.0, 7.0
+    hga.cache_read(cfg, cache, a, b, first, begin)
+    assert torch.equal(a[n - 5:], tail[3:]) and torch.equal(b[n - 5:], -tail[3:])
+    assert bool((a[n - 8:n - 5] == 7).all()) and bool((a[:4] == 5).all()) and bool((b[:4] == 5).all())
+
+
+def test_codes_held_as_bytes_are_the_same_cache():
+    """A pool of uint8 and one of float8_e4m3fn: the same bytes and results."""
+    gen = torch.Generator().manual_seed(32)
+    cfg = _cfg(4, 2, 128, BF)
+    one = _cache(cfg, 1, 6, 6, 16, True, "token")
+    _fill_table(one, [90], gen)
+    two = hga.paged_cache(cfg, one.k.view(torch.uint8).clone(), one.v.view(torch.uint8).clone(), one.page_table,
+                          one.k_scale.clone(), one.v_scale.clone())
+    Q, K = torch.randn(90, 4, 128, generator=gen).to(BF).cuda(), torch.randn(90, 2, 128, generator=gen).to(BF).cuda()
+    got = []
+    for cache in (one, two):
+        hga.cache_write(cfg, cache, K, K, _rows([0, 90]), _rows([0]))
+        O, lse = torch.empty_like(Q), torch.empty(90, 4, device="cuda")
+        ws = torch.empty(hga.paged_workspace_size(cfg, 90), dtype=torch.uint8, device="cuda")
+        hga.attend_paged_fwd(cfg, cache, Q, _rows([0, 90]), _rows([0]), O, lse, ws)
+        got.append((cache.k.view(torch.uint8), cache.v.view(torch.uint8), cache.k_scale, cache.v_scale, O, lse))
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+
+
+@pytest.mark.parametrize("rows", [3, 70])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_the_largest_pages(rows, e4m3):
+    gen = torch.Generator().manual_seed(33)
+    cfg = _cfg(2, 1, 64, BF)
+    cache = _cache(cfg, 1, 2, 3, 65536, e4m3, "head", fill=0xFF)
+    cache.page_table.copy_(torch.tensor([[2, 0]]))
+    ctx = 65536 + 201
+    Kd, Vd = _context(cfg, cache, [ctx], gen, e4m3)
+    Q = torch.randn(rows, 2, 64, generator=gen).to(BF).cuda()
+    _attend_check(cfg, cache, Q, [0, rows], [ctx - rows], Kd, Vd, rows, what="large pages")
