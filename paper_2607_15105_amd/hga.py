@@ -452,11 +452,12 @@ def attend_gathered_bwd(cfg: Config, Q, Kc, Vc, K_act, V_act, act_begin: int, O,
 # Paged key/value cache of many sequences, optionally in 8 bits
 # ---------------------------------------------------------------------------
 
-@dataclass
+@dataclass(frozen=True, eq=False)
 class PagedCache:
     """Device buffers of a paged cache and their descriptor. k, v:
     [n_pages, page_size, Hkv, d] views (any order in memory with d contiguous);
-    k_scale, v_scale: uint8 [n_pages, Hkv, page_size] of an e4m3 cache."""
+    k_scale, v_scale: uint8 [n_pages, Hkv, page_size] of an e4m3 cache. Calls go
+    by the descriptor, so the buffers are written in place, never replaced."""
     k: torch.Tensor
     v: torch.Tensor
     page_table: torch.Tensor
@@ -465,11 +466,9 @@ class PagedCache:
     desc: PagedCacheDesc
 
     def __post_init__(self):
-        self.ref = ctypes.byref(self.desc)
-        self.device = self.k.device
-        self.dtype = self.k.dtype
-        self.heads, self.head_dim = self.k.shape[2:]
-        self.n_seqs = self.desc.n_seqs
+        heads, head_dim = self.k.shape[2:]
+        self.__dict__.update(ref=ctypes.byref(self.desc), device=self.k.device, dtype=self.k.dtype, heads=heads,
+                             head_dim=head_dim, n_seqs=self.desc.n_seqs)
 
 
 def _need(ok: bool, what: str) -> None:

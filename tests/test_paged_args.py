@@ -137,3 +137,24 @@ def test_oracle_of_the_format_matches_the_types_own_rounding():
     y[3:, 1:] = 0
     assert po.held(y)[1].tolist() == [0, 1, 1, -100, -100, 120]
     assert math.isnan(float(po.held(torch.tensor([[1.0, math.inf]]))[0][0, 1]))
+
+
+def test_buffers_are_not_replaced_under_the_descriptor():
+    c = _cfg()
+    k = torch.zeros(4, 64, 2, 128, dtype=torch.bfloat16)
+    cache = hga.paged_cache(c, k, k.clone(), torch.zeros(3, 5, dtype=torch.int32))
+    for name in ("k", "v", "page_table", "k_scale", "v_scale", "desc"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, getattr(cache, name))
+
+
+def test_a_larger_workspace_serves_smaller_calls():
+    """One buffer sized for the largest call is enough for every other."""
+    for hq, hkv in ((1, 1), (8, 4), (8, 2), (32, 4)):
+        c = _cfg(hq=hq, hkv=hkv)
+        rows = (1, 2, 3, 4, 5, 8, 9, 16, 17, 32, 33, 63, 64, 65, 200, 256, 257, 5000)
+        size = {(n, m): hga.paged_workspace_size(c, n, m) for n in rows for m in rows}
+        for (n, m), x in size.items():
+            assert x > 0
+            for (n2, m2), y in size.items():
+                assert n2 > n or m2 > m or y <= x, (hq, hkv, n, m, n2, m2)
