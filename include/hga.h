@@ -484,9 +484,10 @@ hga_status_t hga_attend_gathered_bwd(const hga_config_t* cfg, const void* Q, hga
  *               below 2^32 bytes, token strides below 2^27 bytes.
  *   k_scale, v_scale  HGA_CACHE_E4M3: uint8 [n_pages][Hkv][page_size]; else unused.
  *   page_table  int32 [n_seqs][table_cap]. An entry outside [0, n_pages) is an
- *               absent page, as is a position outside the table (or from 2^31 - 128 on): rows written
- *               there are dropped, rows read from there are zeros, and attention
- *               leaves its positions out. Pages may be shared by sequences.
+ *               absent page, as is a position outside the table (or from 2^31 - 128
+ *               on): rows written there are dropped, rows read from there are
+ *               zeros, and attention leaves its positions out. Pages may be
+ *               shared by sequences.
  *   page_size   a power of two in [16, 65536].
  * Formats:
  *   HGA_CACHE_SAME  rows in cfg->dtype, copied;
@@ -532,7 +533,8 @@ typedef struct {
 /*
  * hga_cache_write - the rows' K and V (cfg->dtype, strides ks / vs, rows
  * [0, n_rows)) into their pages, in the cache's format. Two rows of one call
- * that lie in the same slot of the same page leave either.
+ * that lie in the same slot of the same page leave bytes of either there (the
+ * row itself where they are equal).
  */
 hga_status_t hga_cache_write(const hga_config_t* cfg, const hga_paged_cache_t* cache,
                              const void* K, hga_strides_t ks, const void* V, hga_strides_t vs,
@@ -574,14 +576,19 @@ hga_status_t hga_gather_paged(const hga_config_t* cfg, const hga_paged_cache_t* 
  *   lse        float32 [n_rows][Hq], natural log. A row with nothing to attend
  *              has O = 0 and lse = -inf.
  *   max_rows   the most rows that a sequence of the call has, as far as the caller
- *              knows (n_rows always will do; at least 1). It chooses the kernels and is no
- *              limit: a sequence with more rows is computed all the same.
+ *              knows (n_rows always will do; at least 1). It chooses the kernels
+ *              and is no limit: a sequence with more rows is computed all the same.
  *   workspace  device scratch of hga_paged_workspace_size(cfg, n_rows, max_rows)
  *              bytes; needs no initialisation.
- * Scores, softmax and accumulation in float32; with bf16 inputs P is rounded
- * to bf16 before P.V. The keys of a row are split where that fills the GPU and
- * joined in their order, without atomics: the same call gives the same bits. How they
- * are split depends on the batch, so a row's last float32 bits do.
+ *              It is the call's alone while it runs (captured graphs may share
+ *              one where their replays are ordered).
+ * Scores, softmax and accumulation in float32. With bf16 inputs P enters P.V as a
+ * pair of bf16 values (hi + lo, to about 2^-17) for sequences of few rows, rounded
+ * to bf16 for others (more than 16 rows x query heads of a kv head beside other
+ * sequences, more than 32 otherwise); with float32 inputs it is not rounded. The
+ * keys of a row are split where that fills the GPU and joined in their order,
+ * without atomics: the same call gives the same bits. How they are split depends
+ * on the batch, so a row's last float32 bits do.
  */
 hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache_t* cache,
                                   const void* Q, hga_strides_t qs,

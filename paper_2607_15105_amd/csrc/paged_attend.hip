@@ -4,18 +4,19 @@
 //
 // The rows of a sequence and kv head are folded with its G query heads, so
 // that one reading of K and V serves them all, and taken M folded rows at a
-// time: an item is (sequence, kv head, row tile), a unit of work one 64-key
-// tile of an item. Lengths live on the device; every workgroup counts the
-// units of all sequences, takes an equal share of their concatenation and
-// finds its first unit. Shares differ by one unit at most however ragged the
-// batch is, and a long context of few rows spreads over the whole GPU. An item that lies
-// in one share is finished there; one that several shares cut is left as
-// partial results (unnormalised O with its maximum and sum), which a second
-// kernel joins in the order of the keys: no atomics, the same bits every run.
+// time: an item is (sequence, kv head, row tile), a unit of work 32 or 64 keys
+// of an item. Lengths live on the device; every workgroup counts the units of
+// all sequences, takes an equal share of their concatenation and finds its
+// first unit. However ragged the batch is, the shares are equal, and a long
+// context of few rows spreads over the whole GPU. An item that lies in one
+// share is finished there; one that several shares cut is left as partial
+// results (unnormalised O with its maximum and sum), which a second kernel
+// joins in the order of the keys: no atomics, the same bits every run.
 //
 // Softmax as in the routed kernels: S^T = K . Q^T, every lane holds scores of
-// one row, running maximum and sum per lane, the maximum raised lazily, O^T +=
-// V^T . P^T straight from the score registers.
+// one row, running maximum and sum per lane, the maximum raised lazily (when
+// it grows by over 2^8), O^T += V^T . P^T straight from the score registers;
+// maxima, sums and O are float32.
 #include "paged_device.h"
 
 namespace hga {
@@ -43,7 +44,7 @@ struct SeqShape {
   int shift;      // row tiles hold 2^shift tokens
   bool plain;     // all positions inside [0, cap)
 
-  __device__ inline int nt() const { return (n + (1 << shift) - 1) >> shift; }
+  __device__ inline int nt() const { return ((n - 1) >> shift) + 1; }
   // position of row i, clamped to 32 bits
   __device__ inline int pos(int64_t i) const { return (int)(qb + i < kMaxPos ? qb + i : kMaxPos); }
   // one past the last position that row tile j attends
@@ -98,7 +99,8 @@ struct Share {
   SeqShape<KS> q;   // of sequence s
 };
 
-// NT threads, W workgroups; `lds` holds NT / 64 + 2 int64. A share is a multiple of `step` units, `least` at least.
+// NT threads, W workgroups; `lds` holds NT / 64 + 2 int64. A share is a multiple
+// of `step` units, `least` at least.
 template <int NT, int W, int KS>
 __device__ inline Share<KS> take_share(int wg, int shift, int step, int least, int64_t* lds) {
   constexpr int NW = NT / 64;
@@ -148,8 +150,8 @@ __device__ inline Share<KS> take_share(int wg, int shift, int step, int least, i
     sh.q = shape_of<KS>(a, sh.s, shift);
     const int64_t m = sh.q.units();
     // kv head and rest: 32-bit division where it will do
-    int h = m < ((int64_t)1 << 31) && off < ((int64_t)1 << 31) ? (int)((uint32_t)off / (uint32_t)m) : (int)(off / m);
-    sh.h = __builtin_amdgcn_readfirstlane(h);
+    const bool narrow = m < ((int64_t)1 << 31) && off < ((int64_t)1 << 31);
+    sh.h = __builtin_amdgcn_readfirstlane(narrow ? (int)((uint32_t)off / (uint32_t)m) : (int)(off / m));
     off -= sh.h * m;
     int lo = 0, hi = sh.q.nt() - 1;  // the last row tile that begins at or before off
     while (lo < hi) {
@@ -326,7 +328,7 @@ struct TileRegs {
   static_assert(IPW % IPB == 0, "a wave loads whole blocks of 16 rows");
   static constexpr int BLOCKS = NW == 1 ? KT / 16 : 1;  // blocks of 16 rows of a tensor that the wave loads
   u32x4 w[IPW];
-  uint32_t sc;  // F8, NW == 1: scale byte of K's row `lane`, or V's row lane - KT; else of the wave's row lane % 16
+  uint32_t sc;  // F8: scale byte of K's row `lane`, or V's row lane - KT (NW == 1); of the wave's row lane % 16
 
   // `page`: of the wave's blocks.
   __device__ inline void load(const KvItem& a, int tile, const int (&page)[BLOCKS], int wave, int lane) {
@@ -354,7 +356,8 @@ struct TileRegs {
       const char* base = (v ? a.v : a.k) + ((uint64_t)pg * (v ? a.v_page : a.k_page) + (uint64_t)slot * tok);
 #pragma unroll
       for (int i = 0; i < IPB; ++i)
-        w[b * IPB + i] = *reinterpret_cast<const u32x4*>(base + (uint32_t)((lane / PPR + i * R) * tok + (lane % PPR) * 16));
+        w[b * IPB + i] =
+            *reinterpret_cast<const u32x4*>(base + (uint32_t)((lane / PPR + i * R) * tok + (lane % PPR) * 16));
     }
   }
 
@@ -422,7 +425,8 @@ __device__ inline float not_finite(const char* row, int e) {
 // through again after the loop, and add(position, row) adds it to the rows that do
 // attend it. Rare, and apart from the loop: inside it, it cost the loop its registers.
 template <typename T, int D, int KT, bool F8, typename Add>
-__device__ inline void bad_rows(const KvItem& a, int first, int last, int stride, int sub, int first_pos, int lane, Add&& add) {
+__device__ inline void bad_rows(const KvItem& a, int first, int last, int stride, int sub, int first_pos, int lane,
+                                Add&& add) {
   for (int i = 0, y = first * sub; y < last * sub; i = i + 1 == sub ? 0 : i + 1, y += i ? 1 : (stride - 1) * sub + 1) {
     const uint64_t ok = present<KT>(a, y, lane);
     if (ok == all_keys<KT>() && y * KT + KT - 1 <= first_pos) continue;  // not masked
@@ -461,7 +465,6 @@ struct WaveRows {
   using TL = Tile<T, D>;
   static constexpr int E = EL::E, KS = EL::KSTEP, EB = EL::kBytes;
   static constexpr int NKS = D / KS, NDT = D / 32, VPS = 16 / E;
-  static constexpr int NH = KT / 32;
   using ST = Stage<T, D, KT>;
 
   Frag qf[NKS];
@@ -523,35 +526,25 @@ struct WaveRows {
       for (int dt = 0; dt < NDT; ++dt) oacc[dt] *= corr;
     }
   }
+  // float32: the scores' exponentials, and O^T += V^T . P^T over keys 32 t ... of the stage.
   __device__ __forceinline__ void probs(const f32x16& s, Probs& pf, float c) {
     const float mc = m == -__builtin_inff() ? 0.0f : m * c;  // nothing attended yet: every p is 0
     float sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < VPS; ++k) {
-      float pv[E];
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        pv[j] = __builtin_amdgcn_exp2f(fmaf(s[E * k + j], c, -mc));
-        sum += pv[j];
-      }
-      pf[k] = EL::frag_from(pv);  // bf16: P is rounded to the inputs' precision, as in the routed forward
+      pf[k] = __builtin_amdgcn_exp2f(fmaf(s[k], c, -mc));
+      sum += pf[k];
     }
     l += sum;
   }
-  // O^T += V^T . P^T over keys 32 t ... of the stage.
   __device__ __forceinline__ void values(const Probs& pf, const char* st, int t, int lane) {
-    const int hh = lane >> 5, l32 = lane & 31;
 #pragma unroll
-    for (int k = 0; k < VPS; ++k) {
-      const int kk = t * VPS + k;
+    for (int k = 0; k < VPS; ++k)
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) {
-        Frag vf;
-        if constexpr (ST::TR) vf = tr_frag<TL>(st + ST::kV, 32 * dt, 16 * kk + 4 * hh, 16 * kk + 8 + 4 * hh, lane);
-        else vf = EL::load_frag(st + ST::t_off(32 * dt + l32, KS * kk + E * hh));
+        const Frag vf = EL::load_frag(st + ST::t_off(32 * dt + (lane & 31), KS * (t * VPS + k) + (lane >> 5)));
         oacc[dt] = EL::mma(vf, pf[k], oacc[dt]);
       }
-    }
   }
 
   // Operands of the products to come: the next four steps' (see half()).
@@ -569,9 +562,9 @@ struct WaveRows {
   // such). NKS + NB steps of one product each. The product's operand was read
   // from LDS four steps ahead; beside the first NKS products go the
   // exponentials, beside the others the maximum of sn. The order is fixed by
-  // hand: left to itself the compiler gathers the products and waits for each operand
-  // right after asking for it. fr holds the first operands on entry, and those of the
-  // next call on return, whose K is half tk of stage stk.
+  // hand: left to itself the compiler gathers the products and waits for each
+  // operand right after asking for it. fr holds the first operands on entry, and
+  // those of the next call on return, whose K is half tk of stage stk.
   template <bool MORE, typename Hide>
   __device__ __forceinline__ void half(f32x16& s, f32x16& sn, Frag (&fr)[RING], const char* st, int t, const char* stn,
                                        int tn, const char* stk, int tk, float c, int lane, Hide&& hide_next) {
@@ -657,11 +650,13 @@ __device__ inline float lse_of(float m, float l, float c) {
   return l == 0.0f ? -__builtin_inff() : (m * c + __log2f(l)) * kLn2;
 }
 
-// The workgroup's place in the concatenation of all units: consecutive shares
-// on one XCD (workgroups are dealt round-robin to the eight), whose L2 then holds what they share.
+// The workgroup's place in the concatenation of all units: consecutive shares on
+// one XCD (workgroups are dealt round-robin to the eight), whose L2 then holds
+// what they share (three of four reads of a 2,048-row chunk's keys).
 __device__ inline int share_index() { return (blockIdx.x & 7) * (gridDim.x / 8) + (blockIdx.x >> 3); }
 
-// Follows a share item by item: f(share at the item, tiles of it, whether that is all of it), and the record of the one left unfinished.
+// Follows a share item by item: f(share at the item, tiles of it, whether that
+// is all of it), and the record of the one left unfinished.
 template <int KS, typename F>
 __device__ inline void walk(Share<KS> sh, int wg, int shift, F&& f) {
   if (threadIdx.x == 0) args_here().info[wg] = make_int4(0, 0, 0, 0);
@@ -689,12 +684,8 @@ __device__ inline void walk(Share<KS> sh, int wg, int shift, F&& f) {
   }
 }
 
-}  // namespace
-
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
-
-namespace {
 
 // ---------------------------------------------------------------- few rows
 
@@ -704,12 +695,16 @@ template <typename T> struct Elem16;
 template <> struct Elem16<__bf16> {
   using Frag = bf16x8;
   static constexpr int E = 8, KS = 32;
-  __device__ static inline f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  __device__ static inline f32x4 mma(Frag a, Frag b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
 };
 template <> struct Elem16<float> {
   using Frag = float;
   static constexpr int E = 1, KS = 4;
-  __device__ static inline f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+  __device__ static inline f32x4 mma(Frag a, Frag b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+  }
 };
 
 // NR groups of 16 folded rows: lane l holds (a quarter of the head dim of) row
@@ -772,7 +767,9 @@ struct FewRows {
             if (!((see >> (16 * t + v)) & 1)) s[r][t][v] = -__builtin_inff();
       }
     }
-    Frag pf[NR], plo[NR];  // bf16: P as a pair hi + lo, to about 2^-17, as in the per-query forward
+    // bf16: P as a pair hi + lo, to about 2^-17, as in the per-query forward. The
+    // second product takes 1% of the time here, and O's error is then its rounding's.
+    Frag pf[NR], plo[NR];
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       float mx = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])),
@@ -856,8 +853,12 @@ struct FewRows {
 // one's rows are under way while the other begins or ends an item. A unit is a
 // tile, or two of 8-bit rows, whose loads are under way at once: either way 16 KB a
 // wave and 128 KB a CU, about what the memory's latency takes. 16-row products
-// although the matrix cores have time to spare: it is the instructions beside them that
-// count (with 32 rows, 64 ragged contexts in 8 bits 180 us).
+// although the matrix cores have time to spare: it is the instructions beside
+// them that count (with 32 rows, 64 ragged contexts in 8 bits took 180 us, with 16
+// and P rounded 175). What bounds it: the memory where contexts are long (eight
+// of 131K in 8 bits 381 us, 5.7 TB/s), the starts and ends of items beside it where
+// they are not (64 of 1K to 16K 178 us, 4.9 TB/s), and a chain of round trips for
+// one short context (2K: 10 us, of which 2 are the launch, 1.5 the share, 5 the tile).
 template <typename T, int D, bool F8, int NR>
 __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs) {
   constexpr int UK = few_unit_keys(F8), SUB = (1 << UK) / 32, KT = 32, NW = 4, M = 16 * NR, OP = D + 4;
@@ -889,7 +890,8 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs) {
         if (at == 0) map.fill(kv, u, 0, lane);
         full = (map.full >> at) & 1;
       }
-      const int page[2] = {__builtin_amdgcn_readlane(map.page[2 * i], at), __builtin_amdgcn_readlane(map.page[2 * i + 1], at)};
+      const int page[2] = {__builtin_amdgcn_readlane(map.page[2 * i], at),
+                           __builtin_amdgcn_readlane(map.page[2 * i + 1], at)};
       r[i].load(kv, u * SUB + i, page, 0, lane);
       if (i == SUB - 1) at = (at + 1) & 63;
     };
@@ -982,7 +984,17 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs) {
 // matrix cores and the vector unit busy at once: the next 32 keys' scores beside
 // these' exponentials, then these' P.V beside the next maximum. Tile x + 1 is
 // staged before tile x is begun, so the phases run on across tiles; x + 2 goes
-// to the third stage meanwhile.
+// to the third stage meanwhile. P is rounded to bf16, as in the routed forward (a
+// pair would add half to the products).
+//
+// What bounds it: 2,048 rows of 32 heads at the end of 32K (bf16 rows) take
+// 0.99 to 1.05 ms by the card, 1.02 to 1.07 PFLOP/s (0.87 ms on zeros: the clock
+// falls under the power of products of real values). A product takes 34 cycles
+// of a SIMD and hides about four vector instructions; 32 keys of a wave have 16
+// products, 16 exponentials and some 60 others. Without the staging of tiles it took
+// 0.71 ms on zeros. Longer operand queues, wave priorities, staggered waves and
+// the exponentials spread over both kinds of product changed it by 1% at most;
+// one phase after the other, 1.10 ms.
 template <typename T, int D, bool F8>
 __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
   constexpr int KT = 1 << kPagedTileKeys, NW = 8;
@@ -1053,8 +1065,8 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
     constexpr No no;
     Frag fr[W::RING];
     // Keys of tile y that do not count, where it has such: a branch (its empty asm
-    // keeps it one; as selects it would run in every tile). With a form of the loop
-    // for tiles without masks the accumulators had two places, and 97 registers went to memory.
+    // keeps it one; as selects it would run in every tile). With a form of the loop for
+    // tiles without masks the accumulators had two places, and 97 registers went to memory.
     auto hide = [&](f32x16& s, int y, int t, uint64_t ok) __attribute__((always_inline)) {
       if (masked(y, ok)) {
         asm volatile("");
@@ -1121,7 +1133,8 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
 #pragma unroll
         for (int v4 = 0; v4 < 4; ++v4)
           store4(ost + l32 * OP + (32 * dt + 8 * v4 + 4 * hh) * EB,
-                 f32x4{w.oacc[dt][4 * v4], w.oacc[dt][4 * v4 + 1], w.oacc[dt][4 * v4 + 2], w.oacc[dt][4 * v4 + 3]} * inv,
+                 f32x4{w.oacc[dt][4 * v4], w.oacc[dt][4 * v4 + 1], w.oacc[dt][4 * v4 + 2], w.oacc[dt][4 * v4 + 3]} *
+                     inv,
                  EB == 2);
       float* lse;
       if (l32 < rows && hh == 0) {
@@ -1172,7 +1185,8 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
 // An item that shares w, w + 1, ... cut: its parts in the order of the keys. A
 // workgroup joins eight rows, 32 lanes each: the lanes read 32 parts' maxima and
 // sums at once and hand the weights round, and the parts' rows are read eight
-// at a time. What bounds it is that chain of four round trips.
+// at a time. What bounds it is that chain of four round trips (4 us), and where
+// many rows are cut their bytes (18 us after a 2,048-row chunk's 256 shares).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs one, int one_rows, int n_one, PagedAttnArgs two,
                                                          int two_rows) {  // n_one: workgroups for the first form's parts
