@@ -583,9 +583,9 @@ hga_status_t hga_gather_paged(const hga_config_t* cfg, const hga_paged_cache_t* 
  *              It is the call's alone while it runs (captured graphs may share
  *              one where their replays are ordered).
  * Scores, softmax and accumulation in float32. With bf16 inputs P enters P.V as a
- * pair of bf16 values (hi + lo, to about 2^-17) for sequences of few rows, rounded
- * to bf16 for others (more than 16 rows x query heads of a kv head beside other
- * sequences, more than 32 otherwise); with float32 inputs it is not rounded. The
+ * pair of bf16 values (hi + lo, to about 2^-17) in the kernels for few rows (16 rows
+ * x query heads of a kv head; with d = 64 up to 64 of them where max_rows says
+ * so), rounded to bf16 in the one for many; with float32 inputs it is not rounded. The
  * keys of a row are split where that fills the GPU and joined in their order,
  * without atomics: the same call gives the same bits. How they are split depends
  * on the batch, so a row's last float32 bits do.

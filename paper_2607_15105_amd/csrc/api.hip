@@ -912,26 +912,31 @@ static size_t paged_ws(const hga_config_t* c, int64_t n_rows, PagedForm form) {
   const size_t rows = 2 * (size_t)hga::paged_workgroups(form) * slot_rows(c, n_rows, form);
   return hga::paged_workgroups(form) * sizeof(int4) + rows * (c->head_dim + 2) * sizeof(float);  // a multiple of 16
 }
-// The forms a call runs: of few rows only where no sequence is
-// expected to have more than that form takes at a time; else the form of many
-// rows, and for the sequences of few rows beside them (generation beside a
-// prompt's chunk) that of 16. A form of its own takes whatever there is.
-static int paged_forms(const hga_config_t* c, int64_t n_seqs, int64_t max_rows, PagedForm (&forms)[2]) {
-  const int64_t folded = max_rows < 64 ? max_rows * (c->n_q_heads / c->n_kv_heads) : 64;
-  if (folded <= 32) {
-    forms[0] = folded <= 16 ? PagedForm::kFew16 : PagedForm::kFew32;
-    return 1;
-  }
-  forms[0] = PagedForm::kTile;
+// The forms a call runs, by the most folded rows that a sequence of it has: 16 at
+// a time where that is all; 32 at a time up to a limit; else 256 at a time.
+// Beside the larger ones the sequences of at most 16 have the form of 16 (generation
+// beside a prompt's chunk), unless all have at most 32: a launch more costs more
+// than it gives there. A form alone takes whatever there is.
+// The form of 32 reads K and V once per 32 rows, but leaves no wave without rows
+// (us, 16 sequences of 8,192 keys; 32 against 256 at a time):
+//   d = 128, bf16, 8 kv heads: 32 rows 136 against 118, 48 177 against 116: never;
+//   d = 64, bf16, 2 kv heads: 32 rows 28 against 31, 64 28 against 33, 96 47
+//   against 34; float32: 32 rows 47 against 123, 64 65 against 125, 308 234 against
+//   348, but with 1,500 keys in 8 bits 50 against 36: to 64.
+static int paged_forms(const hga_config_t* c, int64_t n_seqs, int64_t n_rows, int64_t max_rows,
+                       PagedForm (&forms)[2]) {
+  const int64_t rows = max_rows < n_rows ? max_rows : n_rows, folded = rows * (c->n_q_heads / c->n_kv_heads);
+  const int limit = c->head_dim == 64 ? 64 : 16;
+  forms[0] = folded <= 16 ? PagedForm::kFew16 : folded <= limit ? PagedForm::kFew32 : PagedForm::kTile;
   forms[1] = PagedForm::kFew16;
-  return n_seqs > 1 ? 2 : 1;
+  return n_seqs > 1 && folded > (limit > 32 ? 32 : 16) ? 2 : 1;
 }
 
 size_t hga_paged_workspace_size(const hga_config_t* cfg, int64_t n_rows, int64_t max_rows) {
   if (check_cfg(cfg) != HGA_OK || n_rows < 1 || n_rows >= kMaxTokens || max_rows < 1) return 0;
   PagedForm forms[2];
   size_t need = 0;
-  for (int i = 0, n = paged_forms(cfg, 2, max_rows, forms); i < n; ++i) need += paged_ws(cfg, n_rows, forms[i]);
+  for (int i = 0, n = paged_forms(cfg, 2, n_rows, max_rows, forms); i < n; ++i) need += paged_ws(cfg, n_rows, forms[i]);
   return need;
 }
 
@@ -957,12 +962,11 @@ hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache
   a.scale_log2 = eff_scale(cfg) * 1.4426950408889634f;
   PagedForm forms[2];
   hga::PagedAttnArgs args[2];
-  const int n_forms = paged_forms(cfg, cache->n_seqs, max_rows, forms), few_rows = 16 / G;
+  const int n_forms = paged_forms(cfg, cache->n_seqs, n_rows, max_rows, forms), few_rows = 16 / G;
   char* ws = static_cast<char*>(workspace);
   for (int i = 0; i < n_forms; ++i) {
-    const bool tile = forms[i] == PagedForm::kTile;
-    a.min_rows = n_forms == 2 && tile ? few_rows + 1 : 1;
-    a.max_rows = n_forms == 2 && !tile ? few_rows : 0x7fffffff;
+    a.min_rows = n_forms == 2 && i == 0 ? few_rows + 1 : 1;
+    a.max_rows = i == 1 ? few_rows : 0x7fffffff;
     a.slot_rows = slot_rows(cfg, n_rows, forms[i]);
     a.info = reinterpret_cast<int4*>(ws);
     a.part = reinterpret_cast<float*>(a.info + hga::paged_workgroups(forms[i]));
@@ -970,7 +974,11 @@ hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache
     ws += paged_ws(cfg, n_rows, forms[i]);
     args[i] = a;
   }
-  if (hga::launch_attend_paged(args, forms, n_forms, cache->format == HGA_CACHE_E4M3, cfg->dtype == HGA_BF16,
+  // Few rows of few contexts may have 32 parts each or more, which four half waves
+  // join (64 parts 12 -> 7 us; where they are eight, the further workgroups cost 4 us).
+  const bool many = hga::paged_workgroups(forms[0]) >= 32ll * cache->n_seqs * cfg->n_kv_heads;
+  const int split = many && n_forms == 1 && args[0].slot_rows <= 32 ? 4 : 1;
+  if (hga::launch_attend_paged(args, forms, n_forms, split, cache->format == HGA_CACHE_E4M3, cfg->dtype == HGA_BF16,
                                cfg->head_dim, (hipStream_t)stream) != hipSuccess)
     return HGA_ERR_HIP;
   return HGA_OK;

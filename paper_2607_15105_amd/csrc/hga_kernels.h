@@ -228,8 +228,9 @@ constexpr int kPagedTileKeys = 6;
 constexpr int kPagedFewWorkgroups = 512;   // two per CU
 constexpr int kPagedTileWorkgroups = 256;  // one per CU
 constexpr int paged_workgroups(PagedForm f) { return f == PagedForm::kTile ? kPagedTileWorkgroups : kPagedFewWorkgroups; }
-// One form, or two with the sequences divided between them; joined in one launch.
-hipError_t launch_attend_paged(const PagedAttnArgs* a, const PagedForm* form, int n, bool e4m3, bool bf16, int head_dim,
-                               hipStream_t s);
+// One form, or two with the sequences divided between them; joined in one launch,
+// `split` (1 or 4) half waves to a row.
+hipError_t launch_attend_paged(const PagedAttnArgs* a, const PagedForm* form, int n, int split, bool e4m3, bool bf16,
+                               int head_dim, hipStream_t s);
 
 }  // namespace hga

@@ -847,7 +847,8 @@ struct FewRows {
 
 }  // namespace
 
-// Up to 16 NR folded rows per item: the four waves take every fourth unit each,
+// Up to 16 NR folded rows per item (NR = 2 with d = 64 only: with 128 it holds more
+// than the registers do, and the form of 256 rows was faster from 17 rows on): the four waves take every fourth unit each,
 // on the same rows, with LDS of their own and no barrier; their results are
 // joined at the item's end. Tiles of 32 keys, so that two workgroups fit a CU and
 // one's rows are under way while the other begins or ends an item. A unit is a
@@ -988,7 +989,7 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs) {
 // pair would add half to the products).
 //
 // What bounds it: 2,048 rows of 32 heads at the end of 32K (bf16 rows) take
-// 0.99 to 1.05 ms by the card, 1.02 to 1.07 PFLOP/s (0.87 ms on zeros: the clock
+// 0.99 to 1.10 ms by the card, 0.97 to 1.07 PFLOP/s (0.87 ms on zeros: the clock
 // falls under the power of products of real values). A product takes 34 cycles
 // of a SIMD and hides about four vector instructions; 32 keys of a wave have 16
 // products, 16 exponentials and some 60 others. Without the staging of tiles it took
@@ -1182,48 +1183,64 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
 
 // ---------------------------------------------------------------- the joining
 
+// Workgroups for the parts that one share may leave, of 8 / split rows each.
+__host__ __device__ inline int join_groups(const PagedAttnArgs& a, int m_rows, int split) {
+  const int rows = a.slot_rows < m_rows ? a.slot_rows : m_rows, per = 8 / split;
+  return (rows + per - 1) / per;
+}
+
 // An item that shares w, w + 1, ... cut: its parts in the order of the keys. A
-// workgroup joins eight rows, 32 lanes each: the lanes read 32 parts' maxima and
-// sums at once and hand the weights round, and the parts' rows are read eight
-// at a time. What bounds it is that chain of four round trips (4 us), and where
-// many rows are cut their bytes (18 us after a 2,048-row chunk's 256 shares).
-template <typename T, int D>
+// workgroup joins eight rows by half a wave each, or two by `SPLIT` = four each
+// (every fourth part): the lanes read 32 parts' maxima and sums at once and hand
+// the weights round, and the parts' rows are read eight at a time. What bounds it
+// is that chain of four round trips (4 us); where parts are many, several such (a
+// row over 131,072 keys of two kv heads, 256 parts: 13 us by four, 41 by one); and
+// where many rows are cut their bytes (20 us after a 2,048-row chunk's 256 shares).
+// n_one: workgroups for the first form's parts.
+template <typename T, int D, int SPLIT>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs one, int one_rows, int n_one, PagedAttnArgs two,
-                                                         int two_rows) {  // n_one: workgroups for the first form's parts
+                                                         int two_rows) {
   constexpr int EB = Elem<T>::kBytes, V = D / 32;
   typedef float fV __attribute__((ext_vector_type(V)));
   const bool first = (int)blockIdx.x < n_one;
   const PagedAttnArgs& a = first ? one : two;
-  const int m_rows = first ? one_rows : two_rows, groups = ((a.slot_rows < m_rows ? a.slot_rows : m_rows) + 7) / 8;
+  const int m_rows = first ? one_rows : two_rows, groups = join_groups(a, m_rows, SPLIT);
   const int id = first ? blockIdx.x : blockIdx.x - n_one, wg = id / groups;
   const int4 rec = a.info[wg];
   if (rec.x == 0) return;
   const SeqShape<6> q = shape_of<6>(a, rec.y, 0);
   const int64_t nf = (int64_t)q.n << a.gqa_shift, f0 = (int64_t)rec.w * m_rows;
-  const int row = id % groups * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (row >= m_rows || f0 + row >= nf) return;
+  const int half = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int row = id % groups * (8 / SPLIT) + half / SPLIT, begin = half % SPLIT;
+  const bool live = row < m_rows && f0 + row < nf;
+  if (SPLIT == 1 && !live) return;
+  const int parts = SPLIT == 1 || live ? rec.x : 0;  // SPLIT == 1: the same in the whole workgroup
   const float c = a.scale_log2;
   // part k is the share wg + k's: the first one its last item, the others their first
   auto at = [&](int k) { return ((int64_t)(wg + k) * 2 + (k == 0 ? 1 : 0)) * a.slot_rows + row; };
   float M = -__builtin_inff(), L = 0.0f;
   fV o = fV{};
-  for (int k0 = 0; k0 < rec.x; k0 += 32) {
-    const int n = rec.x - k0 < 32 ? rec.x - k0 : 32;
+  auto raise = [&](float m) {
+    if (m > M) {
+      const float f = __builtin_amdgcn_exp2f((M - m) * c);
+      L *= f;
+      o *= f;
+      M = m;
+    }
+  };
+  auto weight = [&](float m) { return m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - M) * c); };
+  for (int k0 = begin; k0 < parts; k0 += 32 * SPLIT) {
+    const int rest = (parts - k0 + SPLIT - 1) / SPLIT, n = rest < 32 ? rest : 32;
     float m = -__builtin_inff(), l = 0.0f;
     if (lane < n) {
-      m = a.part_ml[at(k0 + lane) * 2];
-      l = a.part_ml[at(k0 + lane) * 2 + 1];
+      m = a.part_ml[at(k0 + lane * SPLIT) * 2];
+      l = a.part_ml[at(k0 + lane * SPLIT) * 2 + 1];
     }
     float mx = m;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 32));
-    if (mx > M) {
-      const float f = __builtin_amdgcn_exp2f((M - mx) * c);
-      L *= f;
-      o *= f;
-      M = mx;
-    }
-    const float f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - M) * c);
+    raise(mx);
+    const float f = weight(m);
     l *= f;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) l += __shfl_xor(l, d, 32);
@@ -1232,7 +1249,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs one, int 
       fV x[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        x[i] = *reinterpret_cast<const fV*>(a.part + at(k0 + (k + i < n ? k + i : n - 1)) * D + lane * V);
+        x[i] = *reinterpret_cast<const fV*>(a.part + at(k0 + (k + i < n ? k + i : n - 1) * SPLIT) * D + lane * V);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float w = __shfl(f, k + i < n ? k + i : 0, 32);
@@ -1240,6 +1257,24 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs one, int 
       }
     }
   }
+  if constexpr (SPLIT > 1) {
+    __shared__ fV s_o[8][32];
+    __shared__ float s_m[8], s_l[8];
+    s_o[half][lane] = o;
+    if (lane == 0) {
+      s_m[half] = M;
+      s_l[half] = L;
+    }
+    __syncthreads();
+    if (begin != 0) return;
+    for (int j = 1; j < SPLIT; ++j) {
+      raise(s_m[half + j]);
+      const float f = weight(s_m[half + j]);
+      L += s_l[half + j] * f;
+      o += s_o[half + j][lane] * f;
+    }
+  }
+  if (!live) return;
   o *= L == 0.0f ? 0.0f : 1.0f / L;
   float* lse;
   char* dst = out_row(a, q.first, rec.z, f0 + row, lse) + lane * V * EB;
@@ -1252,31 +1287,32 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs one, int 
 }
 
 template <typename T, int D, bool F8>
-static hipError_t attend_dispatch(const PagedAttnArgs* a, const PagedForm* form, int n, hipStream_t s) {
+static hipError_t attend_dispatch(const PagedAttnArgs* a, const PagedForm* form, int n, int split, hipStream_t s) {
   int join[2] = {0, 0};
   for (int i = 0; i < n; ++i) {
     const dim3 grid(paged_workgroups(form[i]));
     if (form[i] == PagedForm::kFew16) hipLaunchKernelGGL((paged_few_kernel<T, D, F8, 1>), grid, dim3(256), 0, s, a[i]);
-    else if (form[i] == PagedForm::kFew32) hipLaunchKernelGGL((paged_few_kernel<T, D, F8, 2>), grid, dim3(256), 0, s, a[i]);
-    else hipLaunchKernelGGL((paged_tile_kernel<T, D, F8>), grid, dim3(512), 0, s, a[i]);
+    else if (form[i] == PagedForm::kTile) hipLaunchKernelGGL((paged_tile_kernel<T, D, F8>), grid, dim3(512), 0, s, a[i]);
+    else if constexpr (D == 64) hipLaunchKernelGGL((paged_few_kernel<T, D, F8, 2>), grid, dim3(256), 0, s, a[i]);
+    else return hipErrorInvalidValue;  // d = 128 has no form of 32 rows
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int rows = a[i].slot_rows < paged_rows(form[i]) ? a[i].slot_rows : paged_rows(form[i]);
-    join[i] = paged_workgroups(form[i]) * ((rows + 7) / 8);
+    join[i] = paged_workgroups(form[i]) * join_groups(a[i], paged_rows(form[i]), split);
   }
-  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(join[0] + join[1]), dim3(256), 0, s, a[0], paged_rows(form[0]),
-                     join[0], a[n - 1], paged_rows(form[n - 1]));
+  auto* kernel = split == 1 ? paged_join_kernel<T, D, 1> : paged_join_kernel<T, D, 4>;
+  hipLaunchKernelGGL(kernel, dim3(join[0] + join[1]), dim3(256), 0, s, a[0], paged_rows(form[0]), join[0], a[n - 1],
+                     paged_rows(form[n - 1]));
   return hipGetLastError();
 }
 
-hipError_t launch_attend_paged(const PagedAttnArgs* a, const PagedForm* form, int n, bool e4m3, bool bf16, int head_dim,
-                               hipStream_t s) {
+hipError_t launch_attend_paged(const PagedAttnArgs* a, const PagedForm* form, int n, int split, bool e4m3, bool bf16,
+                               int head_dim, hipStream_t s) {
   if (bf16 && head_dim == 128)
-    return e4m3 ? attend_dispatch<__bf16, 128, true>(a, form, n, s) : attend_dispatch<__bf16, 128, false>(a, form, n, s);
+    return e4m3 ? attend_dispatch<__bf16, 128, true>(a, form, n, split, s) : attend_dispatch<__bf16, 128, false>(a, form, n, split, s);
   if (bf16)
-    return e4m3 ? attend_dispatch<__bf16, 64, true>(a, form, n, s) : attend_dispatch<__bf16, 64, false>(a, form, n, s);
+    return e4m3 ? attend_dispatch<__bf16, 64, true>(a, form, n, split, s) : attend_dispatch<__bf16, 64, false>(a, form, n, split, s);
   // float32: head_dim 64
-  return e4m3 ? attend_dispatch<float, 64, true>(a, form, n, s) : attend_dispatch<float, 64, false>(a, form, n, s);
+  return e4m3 ? attend_dispatch<float, 64, true>(a, form, n, split, s) : attend_dispatch<float, 64, false>(a, form, n, split, s);
 }
 
 }  // namespace hga

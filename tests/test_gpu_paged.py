@@ -744,3 +744,45 @@ def test_the_largest_pages(rows, e4m3):
     Kd, Vd = _context(cfg, cache, [ctx], gen, e4m3)
     Q = torch.randn(rows, 2, 64, generator=gen).to(BF).cuda()
     _attend_check(cfg, cache, Q, [0, rows], [ctx - rows], Kd, Vd, rows, what="large pages")
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (F32, 64)])
+@pytest.mark.parametrize("rows", [20, 50, 330])
+def test_chunks_of_every_size_with_absent_pages_and_poisoned_rows(rows, dtype, d, e4m3):
+    """A chunk, a row beside it and an idle sequence; a fifth of the pages absent,
+    NaN in keys and values behind each row."""
+    say(f"[attend] chunk of {rows}, {dtype} {e4m3}")
+    gen = torch.Generator().manual_seed(34)
+    cfg = _cfg(4, 2, d, dtype)
+    n = [rows, 1, 0]
+    ctx = [rows + 411, 130, 0]
+    cache = _cache(cfg, 3, 60, 80, 16, e4m3, "token", fill=0xFF)
+    _fill_table(cache, ctx, gen)
+    Kd, Vd = _context(cfg, cache, ctx, gen, e4m3)
+    cache.page_table[0, 3:9] = -1
+    cache.page_table[1, 1] = 1000
+    cut = rows - 7  # rows behind `cut` of the chunk are poisoned
+    x = torch.ones(7, 2, d)
+    x[2], x[5, 0, 3] = math.nan, math.nan
+    x = x.to(dtype).cuda()
+    hga.cache_write(cfg, cache, x, x, _rows([0, 7, 7, 7]), _rows([ctx[0] - 7, 0, 0]))
+    Q = torch.randn(rows + 1, 4, d, generator=gen).to(dtype).cuda()
+    first, begin = [0, rows, rows + 1, rows + 1], [ctx[0] - rows, ctx[1] - 1, 0]
+    for max_rows in (1, rows):
+        O, lse = torch.zeros_like(Q), torch.zeros(rows + 1, 4, device="cuda")
+        ws = torch.empty(hga.paged_workspace_size(cfg, rows + 1, max_rows), dtype=torch.uint8, device="cuda")
+        hga.attend_paged_fwd(cfg, cache, Q, _rows(first), _rows(begin), O, lse, ws, max_rows)
+        torch.cuda.synchronize()
+        table = cache.page_table.cpu()
+        for s, a, b in ((0, 0, cut), (1, rows, rows + 1)):
+            L = ctx[s] - (7 if s == 0 else 0)
+            entry = table[s][torch.arange(L) // 16]
+            ok = (entry >= 0) & (entry < 80)
+            pos = begin[s] + torch.arange(b - a)
+            o, z, bo, bl = po.attend(Q[a:b].cpu(), torch.where(ok[:, None, None], Kd[s][:L], 0.0),
+                                     torch.where(ok[:, None, None], Vd[s][:L], 0.0), ok, pos, 1 / math.sqrt(d),
+                                     2.0 ** -8 if dtype == BF else 2.0 ** -24)
+            assert bool(((O[a:b].double().cpu() - o).abs() <= bo).all()), (max_rows, s)
+            assert bool(((lse[a:b].double().cpu() - z).abs() <= bl).all()), (max_rows, s)
+        assert bool(torch.isnan(O[cut + 2:rows]).all())  # every later row attends the NaN

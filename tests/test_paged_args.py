@@ -3,6 +3,7 @@ the binding) before anything is launched; and the float64 oracle of its 8-bit
 format against torch's own conversion."""
 
 import ctypes
+import itertools
 import math
 
 import pytest
@@ -150,11 +151,12 @@ def test_buffers_are_not_replaced_under_the_descriptor():
 
 def test_a_larger_workspace_serves_smaller_calls():
     """One buffer sized for the largest call is enough for every other."""
-    for hq, hkv in ((1, 1), (8, 4), (8, 2), (32, 4)):
-        c = _cfg(hq=hq, hkv=hkv)
+    for (hq, hkv), (d, dtype) in itertools.product(((1, 1), (8, 4), (8, 2), (32, 4)),
+                                                   ((128, torch.bfloat16), (64, torch.bfloat16), (64, torch.float32))):
+        c = _cfg(hq=hq, hkv=hkv, d=d, dtype=dtype)
         rows = (1, 2, 3, 4, 5, 8, 9, 16, 17, 32, 33, 63, 64, 65, 200, 256, 257, 5000)
         size = {(n, m): hga.paged_workspace_size(c, n, m) for n in rows for m in rows}
         for (n, m), x in size.items():
             assert x > 0
             for (n2, m2), y in size.items():
-                assert n2 > n or m2 > m or y <= x, (hq, hkv, n, m, n2, m2)
+                assert n2 > n or m2 > m or y <= x, (hq, hkv, d, dtype, n, m, n2, m2)
