@@ -847,10 +847,10 @@ struct FewRows {
 
 }  // namespace
 
-// Up to 16 NR folded rows per item (NR = 2 with d = 64 only: with 128 it holds more
-// than the registers do, and the form of 256 rows was faster from 17 rows on): the four waves take every fourth unit each,
-// on the same rows, with LDS of their own and no barrier; their results are
-// joined at the item's end. Tiles of 32 keys, so that two workgroups fit a CU and
+// Up to 16 NR folded rows per item (NR = 2 with d = 64 only: with 128 the form of
+// 256 rows was faster from 17 rows on): the four waves take every fourth unit
+// each, on the same rows, with LDS of their own and no barrier; their results
+// are joined at the item's end. Tiles of 32 keys, so that two workgroups fit a CU and
 // one's rows are under way while the other begins or ends an item. A unit is a
 // tile, or two of 8-bit rows, whose loads are under way at once: either way 16 KB a
 // wave and 128 KB a CU, about what the memory's latency takes. 16-row products
@@ -1307,12 +1307,10 @@ static hipError_t attend_dispatch(const PagedAttnArgs* a, const PagedForm* form,
 
 hipError_t launch_attend_paged(const PagedAttnArgs* a, const PagedForm* form, int n, int split, bool e4m3, bool bf16,
                                int head_dim, hipStream_t s) {
-  if (bf16 && head_dim == 128)
-    return e4m3 ? attend_dispatch<__bf16, 128, true>(a, form, n, split, s) : attend_dispatch<__bf16, 128, false>(a, form, n, split, s);
-  if (bf16)
-    return e4m3 ? attend_dispatch<__bf16, 64, true>(a, form, n, split, s) : attend_dispatch<__bf16, 64, false>(a, form, n, split, s);
-  // float32: head_dim 64
-  return e4m3 ? attend_dispatch<float, 64, true>(a, form, n, split, s) : attend_dispatch<float, 64, false>(a, form, n, split, s);
+  auto* f = bf16 && head_dim == 128 ? (e4m3 ? attend_dispatch<__bf16, 128, true> : attend_dispatch<__bf16, 128, false>)
+            : bf16                  ? (e4m3 ? attend_dispatch<__bf16, 64, true> : attend_dispatch<__bf16, 64, false>)
+                                    : (e4m3 ? attend_dispatch<float, 64, true> : attend_dispatch<float, 64, false>);
+  return f(a, form, n, split, s);  // float32: head_dim 64
 }
 
 }  // namespace hga
