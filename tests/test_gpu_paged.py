@@ -786,3 +786,20 @@ def test_chunks_of_every_size_with_absent_pages_and_poisoned_rows(rows, dtype, d
             assert bool(((O[a:b].double().cpu() - o).abs() <= bo).all()), (max_rows, s)
             assert bool(((lse[a:b].double().cpu() - z).abs() <= bl).all()), (max_rows, s)
         assert bool(torch.isnan(O[cut + 2:rows]).all())  # every later row attends the NaN
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(11, 11, 128, BF), (34, 17, 64, BF), (13, 13, 64, F32)])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_many_odd_heads(hq, hkv, d, dtype, e4m3):
+    gen = torch.Generator().manual_seed(35)
+    cfg = _cfg(hq, hkv, d, dtype)
+    ctx, rows = [140, 37], [33, 1]
+    cache = _cache(cfg, 2, 5, 13, 32, e4m3, "token", fill=0xFF)
+    _fill_table(cache, ctx, gen)
+    Kd, Vd = _context(cfg, cache, ctx, gen, e4m3)
+    out = torch.empty(2, 177, hkv, d, dtype=dtype, device="cuda")
+    hga.cache_read(cfg, cache, out[0], out[1], _rows([0, 140, 177]), _rows([0, 0]))
+    assert torch.equal(out[0].double().cpu(), torch.cat(Kd)) and torch.equal(out[1].double().cpu(), torch.cat(Vd))
+    Q = torch.randn(34, hq, d, generator=gen).to(dtype).cuda()
+    for max_rows in (1, 33):
+        _attend_check(cfg, cache, Q, [0, 33, 34], [107, 36], Kd, Vd, max_rows, what=f"{hkv} kv heads")
