@@ -7,7 +7,7 @@
 // time: an item is (sequence, kv head, row tile), a unit of work 32 or 64 keys
 // of an item. Lengths live on the device; every workgroup counts the units of
 // all sequences, takes an equal share of their concatenation and finds its
-// first unit. However ragged the batch is, the shares are equal, and a long
+// first unit. However ragged the batch is, the shares are alike, and a long
 // context of few rows spreads over the whole GPU. An item that lies in one
 // share is finished there; one that several shares cut is left as partial
 // results (unnormalised O with its maximum and sum), which a second kernel
@@ -74,7 +74,12 @@ struct SeqShape {
     }
     return q * (a * (a - 1) / 2) + a * period + rest + a * b;
   }
-  __device__ inline int64_t units() const { return n == 0 ? 0 : before(nt() - 1) + tiles(nt() - 1); }
+  // With `over` units ahead of each item's for its start and end: where item j's
+  // begin, and all of them.
+  __device__ inline int64_t start(int j, int over) const { return before(j) + (int64_t)j * over; }
+  __device__ inline int64_t units(int over) const {
+    return n == 0 ? 0 : start(nt() - 1, over) + over + tiles(nt() - 1);
+  }
 };
 
 template <int KS>
@@ -95,13 +100,17 @@ template <int KS>
 struct Share {
   int64_t left, per;
   int s, h, j;
-  int kt;           // first unit within the item
+  int kt;           // first unit within the item; below zero: so many of its start are left
   SeqShape<KS> q;   // of sequence s
 };
 
 // NT threads, W workgroups; `lds` holds NT / 64 + 2 int64. A share is a multiple
-// of `step` units, `least` at least.
-template <int NT, int W, int KS>
+// of `step` units, `least` at least. An item counts as OVER units more than it
+// has, about what its start and end take, so that shares of many short items are
+// not the last to end. (Not for few rows: four units there made 64 ragged contexts
+// 179 -> 171 us, but eight equal ones of 131K 381 -> 388, and sixteen of 1,000
+// positions, which fill the shares evenly without, 20 -> 25.)
+template <int NT, int W, int KS, int OVER>
 __device__ inline Share<KS> take_share(int wg, int shift, int step, int least, int64_t* lds) {
   constexpr int NW = NT / 64;
   const PagedAttnArgs& a = args_here();
@@ -110,7 +119,7 @@ __device__ inline Share<KS> take_share(int wg, int shift, int step, int least, i
   int64_t sum = 0;
   for (int k = 0; k < c; ++k) {
     const int s = tid * c + k;
-    if (s < n_seqs) sum += a.p.n_kv_heads * shape_of<KS>(a, s, shift).units();
+    if (s < n_seqs) sum += a.p.n_kv_heads * shape_of<KS>(a, s, shift).units(OVER);
   }
   int64_t inc = sum;
 #pragma unroll
@@ -135,7 +144,7 @@ __device__ inline Share<KS> take_share(int wg, int shift, int step, int least, i
   if (sh.left > 0 && off >= 0 && off < sum) {  // this thread's sequences hold the first unit
     int s = tid * c;
     for (; s < n_seqs - 1; ++s) {
-      const int64_t m = a.p.n_kv_heads * shape_of<KS>(a, s, shift).units();
+      const int64_t m = a.p.n_kv_heads * shape_of<KS>(a, s, shift).units(OVER);
       if (off < m) break;
       off -= m;
     }
@@ -148,7 +157,7 @@ __device__ inline Share<KS> take_share(int wg, int shift, int step, int least, i
     sh.s = __builtin_amdgcn_readfirstlane((int)lds[NW]);
     off = lds[NW + 1];
     sh.q = shape_of<KS>(a, sh.s, shift);
-    const int64_t m = sh.q.units();
+    const int64_t m = sh.q.units(OVER);
     // kv head and rest: 32-bit division where it will do
     const bool narrow = m < ((int64_t)1 << 31) && off < ((int64_t)1 << 31);
     sh.h = __builtin_amdgcn_readfirstlane(narrow ? (int)((uint32_t)off / (uint32_t)m) : (int)(off / m));
@@ -156,11 +165,11 @@ __device__ inline Share<KS> take_share(int wg, int shift, int step, int least, i
     int lo = 0, hi = sh.q.nt() - 1;  // the last row tile that begins at or before off
     while (lo < hi) {
       const int mid = (int)(((int64_t)lo + hi + 1) >> 1);
-      if (sh.q.before(mid) <= off) lo = mid;
+      if (sh.q.start(mid, OVER) <= off) lo = mid;
       else hi = mid - 1;
     }
     sh.j = __builtin_amdgcn_readfirstlane(lo);
-    sh.kt = __builtin_amdgcn_readfirstlane((int)(off - sh.q.before(sh.j)));
+    sh.kt = __builtin_amdgcn_readfirstlane((int)(off - sh.q.start(sh.j, OVER)) - OVER);
   }
   __syncthreads();
   return sh;
@@ -657,10 +666,15 @@ __device__ inline int share_index() { return (blockIdx.x & 7) * (gridDim.x / 8) 
 
 // Follows a share item by item: f(share at the item, tiles of it, whether that
 // is all of it), and the record of the one left unfinished.
-template <int KS, typename F>
+template <int OVER, int KS, typename F>
 __device__ inline void walk(Share<KS> sh, int wg, int shift, F&& f) {
   if (threadIdx.x == 0) args_here().info[wg] = make_int4(0, 0, 0, 0);
   while (sh.left > 0) {
+    if (OVER > 0 && sh.kt < 0) {
+      sh.left += sh.kt;
+      sh.kt = 0;
+      if (sh.left <= 0) return;  // the item is the next share's
+    }
     const int len = sh.q.tiles(sh.j), rest = len - sh.kt;
     const int n = rest < sh.left ? rest : (int)sh.left;
     if (sh.kt == 0 && n < len) {  // goes on in the next shares: this one joins it
@@ -669,7 +683,7 @@ __device__ inline void walk(Share<KS> sh, int wg, int shift, F&& f) {
     }
     f(sh, n, n == len);
     sh.left -= n;
-    sh.kt = 0;
+    sh.kt = -OVER;
     if (sh.left > 0 && ++sh.j == sh.q.nt()) {
       const PagedAttnArgs& a = args_here();
       sh.j = 0;
@@ -870,10 +884,10 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs) {
   __shared__ int64_t s_scan[NW + 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int shift = (NR == 1 ? 4 : 5) - args_here().gqa_shift, wg = share_index();
-  const Share<UK> share = take_share<256, kPagedFewWorkgroups, UK>(wg, shift, NW, NW, s_scan);
+  const Share<UK> share = take_share<256, kPagedFewWorkgroups, UK, 0>(wg, shift, NW, NW, s_scan);
   const float c = args_here().scale_log2;
   char* st = smem + wave * SB;
-  walk(share, wg, shift, [&](const Share<UK>& sh, int n, bool whole) {
+  walk<0>(share, wg, shift, [&](const Share<UK>& sh, int n, bool whole) {
     const SeqShape<UK>& q = sh.q;
     const PagedAttnArgs& a0 = args_here();
     const int first_pos = q.pos((int64_t)sh.j << shift);
@@ -1005,17 +1019,20 @@ __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
   // the least share, in units: what a unit takes (bf16 2 us, float32 7) against a
   // partial result's writing and joining
   constexpr int kLeast = sizeof(T) == 2 ? 4 : 1;
+  // units for an item's start and end (about 6 us): a prompt of 8,192 rows from its
+  // beginning 695 us with none, 645 with two, 622 with three
+  constexpr int kOver = sizeof(T) == 2 ? 3 : 1;
   __shared__ __attribute__((aligned(16))) char smem[3 * SB];
   __shared__ int64_t s_scan[NW + 2];
   __shared__ int s_bad[2];  // whether V had what is not finite in this item, and in the next
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int shift = kPagedTileRowsLog2 - args_here().gqa_shift, wg = share_index();
-  const Share<kPagedTileKeys> share = take_share<512, kPagedTileWorkgroups, kPagedTileKeys>(wg, shift, 1, kLeast, s_scan);
+  const Share<kPagedTileKeys> share = take_share<512, kPagedTileWorkgroups, kPagedTileKeys, kOver>(wg, shift, 1, kLeast, s_scan);
   const float c = args_here().scale_log2;
   if (tid < 2) s_bad[tid] = 0;
   __syncthreads();
   int item = 0;
-  walk(share, wg, shift, [&](const Share<kPagedTileKeys>& sh, int n, bool whole) {
+  walk<kOver>(share, wg, shift, [&](const Share<kPagedTileKeys>& sh, int n, bool whole) {
     const SeqShape<kPagedTileKeys>& q = sh.q;
     const PagedAttnArgs& a0 = args_here();
     const int first_pos = q.pos((int64_t)sh.j << shift);
