@@ -496,8 +496,10 @@ hga_status_t hga_attend_gathered_bwd(const hga_config_t* cfg, const void* Q, hga
  *               integer >= -100 with max |x_j| <= 448 * 2^e over the finite x_j,
  *               held as the byte e + 127; the codes are x_j / 2^e, an exact
  *               quotient, rounded to nearest even: x_j is held within 2^-4
- *               relative, or within 2^(e-10) where it is below 2^(e-6). NaN and
- *               infinities are held as NaN. A held value is exact in bf16.
+ *               relative, or within 2^(e-10) where it is below 2^(e-6). A finite
+ *               x_j over 240 * 2^120 in magnitude, whose code would round to
+ *               256 * 2^120 = 2^128, is held as 240 * 2^120 (within 2^-4 too).
+ *               NaN and infinities are held as NaN. A held value is exact in bf16.
  *
  * The calls below take the rows of a ragged batch: rows [seq_rows[s],
  * seq_rows[s + 1]) of n_rows belong to sequence s and are its positions

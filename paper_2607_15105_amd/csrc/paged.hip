@@ -103,6 +103,7 @@ __global__ __launch_bounds__(256) void cache_write_kernel(PagedArgs a, DenseRows
 #pragma unroll
           for (int o = LPR / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
           const int e = row_exponent(m);
+          cap_values<N>(x, e);
           const float inv = exp2i(-e);
           if constexpr (N == 8) {
             const u32x2 y = {codes4(x, inv), codes4(x + 4, inv)};

@@ -1,0 +1,80 @@
+"""GPU checks of the paged cache at the ends of the values' range: the largest
+finite ones through the 8-bit format, against float64 on the CPU."""
+
+import math
+
+import pytest
+import torch
+
+from paper_2607_15105_amd import hga
+from tests import paged_oracle as po
+from tests.test_gpu_paged import BF, F32, _attend_check, _cache, _cfg, _fill_table, _held_rows, _rows, say
+
+pytestmark = pytest.mark.gpu
+
+TOP = 240 * 2.0 ** 120  # the largest value of four significant bits below 2^128
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    hga.lib()
+
+
+# ---------------------------------------------------------------- the largest finite values in 8 bits
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 64)])
+@pytest.mark.parametrize("layout", ["head", "token"])
+def test_the_largest_finite_values_stay_finite(dtype, d, layout):
+    """Rows whose largest magnitude lies around 224, 240 and 248 times 2^120 and at
+    the type's maximum: held as the values up to TOP are, those over it as TOP."""
+    say(f"[write, read] largest values, {dtype}, d {d}, {layout}")
+    gen = torch.Generator().manual_seed(41)
+    cfg = _cfg(2, 2, d, dtype)
+    tops = [torch.finfo(dtype).max, 255 * 2.0 ** 120, 249 * 2.0 ** 120, 248 * 2.0 ** 120, 247 * 2.0 ** 120,
+            241 * 2.0 ** 120, TOP, 232 * 2.0 ** 120, 225 * 2.0 ** 120, 224 * 2.0 ** 120, 223 * 2.0 ** 120]
+    n = 2 * len(tops)
+    x = torch.randn(n, 2, d, generator=gen) * 2.0 ** 118
+    for i, v in enumerate(tops):
+        x[2 * i, :, 3], x[2 * i + 1, :, 7] = v, -v
+        x[2 * i, 1, 20:28] = torch.tensor(tops[:8]).clamp(max=v)  # several of them in one row
+    x = x.to(dtype)
+    cache = _cache(cfg, 1, 4, 4, 16, True, layout)
+    _fill_table(cache, [n], gen)
+    hga.cache_write(cfg, cache, x.cuda(), -x.cuda(), _rows([0, n]), _rows([0]))
+    out = torch.full((2, n, 2, d), 7.0, dtype=dtype, device="cuda")
+    hga.cache_read(cfg, cache, out[0], out[1], _rows([0, n]), _rows([0]))
+    torch.cuda.synchronize()
+    exact = x.double()
+    code, e = po.held(exact.clamp(-TOP, TOP))
+    want = code * torch.exp2(e)[..., None]
+    assert bool(torch.isfinite(want).all()) and bool((want.abs() <= TOP).all())
+    # the promise about them: 2^-4 relative, or 2^(e - 10) where that is more
+    assert bool(((want - exact).abs() <= torch.maximum(exact.abs() * 2.0 ** -4, torch.exp2(e - 10)[..., None])).all())
+    for sign, got in ((1.0, out[0]), (-1.0, out[1])):
+        assert torch.equal(sign * got.double().cpu(), want), float(got.float().abs().max())
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 64)])
+@pytest.mark.parametrize("max_rows", [1, 5, 140])
+def test_attention_of_the_largest_finite_values(dtype, d, max_rows):
+    """Values of the type's maximum at keys of weight e^-5 beside others, in tiles
+    that are masked for some of the rows and not for others."""
+    say(f"[attend] largest values, {dtype}, d {d}, max_rows {max_rows}")
+    gen = torch.Generator().manual_seed(42)
+    cfg = _cfg(4, 2, d, dtype)
+    ctx, rows = 300, 140
+    cache = _cache(cfg, 1, 20, 20, 16, True, "head")
+    _fill_table(cache, [ctx], gen)
+    K, V = torch.zeros(ctx, 2, d), torch.randn(ctx, 2, d, generator=gen)
+    top = torch.finfo(dtype).max
+    for t, h, i, v in ((3, 0, 5, top), (70, 1, 6, -top), (200, 0, 7, top), (201, 1, 8, -top)):
+        K[t, h] = -5.0 / math.sqrt(d)
+        V[t, h, i] = v
+    K, V = K.to(dtype), V.to(dtype)
+    hga.cache_write(cfg, cache, K.cuda(), V.cuda(), _rows([0, ctx]), _rows([0]))
+    Kd, Vd = (_held_rows(cfg, x.double().clamp(-TOP, TOP), True) for x in (K, V))
+    Q = torch.ones(rows, 4, d, dtype=dtype, device="cuda")
+    O, _ = _attend_check(cfg, cache, Q, [0, rows], [ctx - rows], [Kd], [Vd], max_rows, what="largest values")
+    assert bool(torch.isfinite(O).all()) and float(O.float().abs().max()) > 1e30
