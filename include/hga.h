@@ -571,7 +571,9 @@ hga_status_t hga_gather_paged(const hga_config_t* cfg, const hga_paged_cache_t* 
  * page is present, its own and the batch's earlier rows among them (written by
  * hga_cache_write before). One call serves decode steps (one row per sequence),
  * chunks of a prompt, and both in one batch. Keys after a row never enter its
- * result, infinities and NaN among them.
+ * result, infinities and NaN among them. An infinity in V makes the elements of
+ * the rows that attend it infinite, or NaN: where it meets NaN or an infinity of
+ * the other sign, or has a weight of zero in float32.
  *
  *   Q          rows [0, n_rows) of cfg->dtype, strides qs.
  *   O          rows [0, n_rows) of cfg->dtype, strides os (bf16 rounded to nearest even).

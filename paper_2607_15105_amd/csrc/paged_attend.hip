@@ -428,22 +428,37 @@ __device__ inline float not_finite(const char* row, int e) {
   return fabsf(x) < __builtin_inff() ? 0.0f : x;
 }
 
+// Whether a held row of V is finite.
+template <typename T, int D, bool F8>
+__device__ inline bool finite_row(const char* row) {
+  bool fine = true;
+#pragma unroll 1
+  for (int i = 0; i < D * (F8 ? 1 : Elem<T>::kBytes) / 16; ++i) {
+    const uint4 w = *reinterpret_cast<const uint4*>(row + 16 * i);
+    if constexpr (F8) {
+      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+      for (int j = 0; j < 16; ++j) fine = fine && ((u[j >> 2] >> (8 * (j & 3))) & 0x7f) != 0x7f;
+    } else {
+      fine = fine && finite16<T>(w);
+    }
+  }
+  return fine;
+}
+
 // What is not finite in V is left out of masked tiles (a product with p = 0
 // would bring it to rows that do not attend its key). Where there was such, the
 // units first, first + stride, ... before `last`, of `sub` tiles each, are looked
-// through again after the loop, and add(position, row) adds it to the rows that do
-// attend it. Rare, and apart from the loop: inside it, it cost the loop its registers.
+// through again after the loop, the masked tiles or all of them, and add(position,
+// row) adds it to the rows that do attend it. Rare, and apart from the loop: inside
+// it, it cost the loop its registers.
 template <typename T, int D, int KT, bool F8, typename Add>
-__device__ inline void bad_rows(const KvItem& a, int first, int last, int stride, int sub, int first_pos, int lane,
-                                Add&& add) {
+__device__ inline void bad_rows(const KvItem& a, int first, int last, int stride, int sub, int first_pos, bool all,
+                                int lane, Add&& add) {
   for (int i = 0, y = first * sub; y < last * sub; i = i + 1 == sub ? 0 : i + 1, y += i ? 1 : (stride - 1) * sub + 1) {
     const uint64_t ok = present<KT>(a, y, lane);
-    if (ok == all_keys<KT>() && y * KT + KT - 1 <= first_pos) continue;  // not masked
+    if (!all && ok == all_keys<KT>() && y * KT + KT - 1 <= first_pos) continue;  // not masked
     bool fine = true;
-    if ((ok >> lane) & 1) {  // a row per lane
-      const char* row = a.v_row(y * KT + lane);
-      for (int e = 0; e < D; ++e) fine = fine && not_finite<T, F8>(row, e) == 0.0f;
-    }
+    if ((ok >> lane) & 1) fine = finite_row<T, D, F8>(a.v_row(y * KT + lane));  // a row per lane
     uint64_t bad = __ballot(!fine);
     while (bad) {
       const int t = y * KT + __builtin_ctzll(bad);
@@ -626,7 +641,7 @@ struct WaveRows {
 
   template <bool F8>
   __device__ inline void add_bad(const KvItem& a, int first, int last, int first_pos, int lane) {
-    bad_rows<T, D, KT, F8>(a, first, last, 1, 1, first_pos, lane, [&](int t, const char* row) {
+    bad_rows<T, D, KT, F8>(a, first, last, 1, 1, first_pos, false, lane, [&](int t, const char* row) {
       if (pos < t) return;
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
@@ -844,16 +859,49 @@ struct FewRows {
     }
   }
 
+  // bf16: whether the products left O finite. An infinity of V is one by P's high half,
+  // but NaN by a low half of zero, or by one of the other sign.
+  __device__ __forceinline__ bool finite() const {
+    float z = 0.0f;
+    if constexpr (EB == 2) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) z = fmaf(oacc[r][dt][v], 0.0f, z);
+    }
+    return !__any(z != 0.0f);
+  }
+
+  // Adds what masked tiles left out, and puts it in the place of what the products made
+  // of it in the others.
   template <bool F8>
   __device__ inline void add_bad(const KvItem& a, int first, int last, int stride, int sub, int first_pos, int lane) {
-    bad_rows<T, D, 32, F8>(a, first, last, stride, sub, first_pos, lane, [&](int t, const char* row) {
+    static_assert(NR * NDT * 4 <= 32, "a bit for each element");
+    uint32_t spoilt = 0;
+    if constexpr (EB == 2) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (!(fabsf(oacc[r][dt][v]) < __builtin_inff())) spoilt |= 1u << ((r * NDT + dt) * 4 + v);
+    }
+    bad_rows<T, D, 32, F8>(a, first, last, stride, sub, first_pos, __any(spoilt != 0), lane, [&](int t, const char* row) {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           const float x = not_finite<T, F8>(row, 16 * dt + 4 * (lane >> 4) + v);
 #pragma unroll
-          for (int r = 0; r < NR; ++r) oacc[r][dt][v] += pos[r] < t ? 0.0f : x;
+          for (int r = 0; r < NR; ++r) {
+            if (x == 0.0f || pos[r] < t) continue;
+            const uint32_t bit = 1u << ((r * NDT + dt) * 4 + v);
+            oacc[r][dt][v] = spoilt & bit ? x : oacc[r][dt][v] + x;
+            spoilt &= ~bit;
+          }
         }
     });
   }
@@ -939,7 +987,7 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs) {
 #pragma unroll
       for (int i = 0; i < SUB; ++i) tile(i, No());
     }
-    if (bad) w.template add_bad<F8>(kv, x0, last, NW, SUB, first_pos, lane);
+    if (bad || !w.finite()) w.template add_bad<F8>(kv, x0, last, NW, SUB, first_pos, lane);
     // join the waves: rows as [wave][row][D] through the stages
     const PagedAttnArgs& a = args_here();
     __syncthreads();

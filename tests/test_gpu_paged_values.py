@@ -1,5 +1,6 @@
 """GPU checks of the paged cache at the ends of the values' range: the largest
-finite ones through the 8-bit format, against float64 on the CPU."""
+finite ones through the 8-bit format, and what is not finite in V where it is
+attended, in tiles with and without masks, against float64 on the CPU."""
 
 import math
 
@@ -8,7 +9,7 @@ import torch
 
 from paper_2607_15105_amd import hga
 from tests import paged_oracle as po
-from tests.test_gpu_paged import BF, F32, _attend_check, _cache, _cfg, _fill_table, _held_rows, _rows, say
+from tests.test_gpu_paged import BF, F32, _attend_check, _cache, _cfg, _context, _fill_table, _held_rows, _rows, say
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +79,62 @@ def test_attention_of_the_largest_finite_values(dtype, d, max_rows):
     Q = torch.ones(rows, 4, d, dtype=dtype, device="cuda")
     O, _ = _attend_check(cfg, cache, Q, [0, rows], [ctx - rows], [Kd], [Vd], max_rows, what="largest values")
     assert bool(torch.isfinite(O).all()) and float(O.float().abs().max()) > 1e30
+
+
+# ---------------------------------------------------------------- what is not finite in V, where it is attended
+
+def _attend_not_finite(cfg, cache, Q, begin, Kd, Vd, max_rows, what):
+    """One sequence's rows over K, V [L, Hkv, d] in float64, V with infinities and
+    NaN. Of an element of O whose attended values are not all finite the result is
+    their sum: an infinity, or NaN; the others are held to their bounds."""
+    n, Hq, d = Q.shape
+    G = Hq // Kd.shape[1]
+    O, lse = torch.full_like(Q, 7.0), torch.full((n, Hq), 7.0, device="cuda")
+    ws = torch.full((hga.paged_workspace_size(cfg, n, max_rows),), 255, dtype=torch.uint8, device="cuda")
+    hga.attend_paged_fwd(cfg, cache, Q, _rows([0, n]), _rows([begin]), O, lse, ws, max_rows)
+    torch.cuda.synchronize()
+    pos = begin + torch.arange(n)
+    fine = torch.isfinite(Vd)
+    o, z, bo, bl = po.attend(Q.cpu(), Kd, torch.where(fine, Vd, 0.0), torch.ones(len(Kd), dtype=torch.bool), pos,
+                             1 / math.sqrt(d), 2.0 ** -8 if Q.dtype == BF else 2.0 ** -24)
+    odd = torch.zeros(n, Hq, d, dtype=torch.float64)
+    for t in torch.nonzero((~fine).flatten(1).any(1))[:, 0].tolist():
+        x = torch.where(fine[t], 0.0, Vd[t]).repeat_interleave(G, 0)
+        odd = odd + torch.where((pos >= t)[:, None, None], x, 0.0)
+    got = O.double().cpu()
+    some = odd != 0  # NaN too
+    assert int(some.sum()) > 0 and bool((~some).any())
+    same = (got == odd) | (torch.isnan(got) & torch.isnan(odd))
+    wrong = torch.nonzero(some & ~same)
+    assert len(wrong) == 0, (what, len(wrong), [(i.tolist(), float(got[tuple(i)]), float(odd[tuple(i)])) for i in wrong[:4]])
+    assert bool(((got - o).abs() <= bo)[~some].all()), what
+    assert bool(((lse.double().cpu() - z).abs() <= bl).all()), what
+
+
+@pytest.mark.parametrize("dtype,d,heads", [(BF, 128, (4, 2)), (BF, 64, (8, 2)), (F32, 64, (4, 2))])
+@pytest.mark.parametrize("ctx,rows", [(300, 140), (3000, 3), (3000, 9), (9000, 70)])
+@pytest.mark.parametrize("expected", ["one", "all"])
+def test_infinities_in_attended_values(dtype, d, heads, ctx, rows, expected):
+    """Infinities and NaN in V of rows that are held as they are, at the beginning, in
+    the middle and among the new rows: the same result whether a tile is masked, and in
+    every form."""
+    say(f"[attend] infinite values, {dtype}, d {d}, {rows} rows over {ctx}, {expected}")
+    gen = torch.Generator().manual_seed(43)
+    cfg = _cfg(*heads, d, dtype)
+    cache = _cache(cfg, 1, -(-ctx // 32), -(-ctx // 32), 32, False, "token")
+    _fill_table(cache, [ctx], gen)
+    Kd, Vd = _context(cfg, cache, [ctx], gen, False)
+    bad = torch.full((ctx, heads[1], d), math.nan, dtype=torch.float64)  # NaN: as it is
+    inf, begin = math.inf, ctx - rows
+    for t, h, i, v in ((0, 0, 1, inf), (33, 1, 2, -inf), (ctx // 2, 0, 3, inf), (ctx // 2 + 1, 0, 3, -inf),
+                       (ctx // 2 + 1, 1, 4, inf), (begin - 1, 0, 5, -inf), (begin, 1, d - 1, inf),
+                       (begin + rows // 2, 0, d - 2, -inf), (ctx - 1, 1, d - 3, inf), (64, 1, 2, -inf)):
+        bad[t, h, i] = v
+        Vd[0][t, h, i] = v
+    Vd[0][40, 1, 9] = math.nan  # one NaN, early
+    at = torch.nonzero(~torch.isnan(bad) | torch.isnan(Vd[0]))
+    page = cache.page_table[0].cpu()
+    for t, h, i in at.tolist():
+        cache.v[int(page[t // 32]), t % 32, h, i] = float(Vd[0][t, h, i])
+    Q = torch.randn(rows, heads[0], d, generator=gen).to(dtype).cuda()
+    _attend_not_finite(cfg, cache, Q, begin, Kd[0], Vd[0], 1 if expected == "one" else rows, "infinities")
