@@ -500,6 +500,8 @@ hga_status_t hga_attend_gathered_bwd(const hga_config_t* cfg, const void* Q, hga
  *               x_j over 240 * 2^120 in magnitude, whose code would round to
  *               256 * 2^120 = 2^128, is held as 240 * 2^120 (within 2^-4 too).
  *               NaN and infinities are held as NaN. A held value is exact in bf16.
+ *               (A pool that the caller fills may hold codes and scales that stand
+ *               for 2^128 and more: they count as infinities.)
  *
  * The calls below take the rows of a ragged batch: rows [seq_rows[s],
  * seq_rows[s + 1]) of n_rows belong to sequence s and are its positions

@@ -199,6 +199,10 @@ struct KvItem {
 
   // V's row of position t, which is present.
   __device__ inline const char* v_row(int t) const { return v + page_off(table[t >> shift], t & mask, v_page, v_tok); }
+  // Its scale, of 8-bit rows.
+  __device__ inline float v_row_scale(int t) const {
+    return __uint_as_float((uint32_t)v_scale[(uint64_t)(uint32_t)table[t >> shift] * scale_page + (uint32_t)(t & mask)] << 23);
+  }
 };
 
 // Where 64 tiles of an item lie: lane i has the pages of tile x0 + i * STRIDE, a tile
@@ -418,11 +422,12 @@ struct TileRegs {
   }
 };
 
-// Element e of a held row of V where it is not finite, else 0.
+// Element e of a held row of V where it is not finite, else 0: judged by its value, as
+// the tiles' rows are (8 bits: a code and its scale may stand for 2^128 and more).
 template <typename T, bool F8>
-__device__ inline float not_finite(const char* row, int e) {
+__device__ inline float not_finite(const char* row, float scale, int e) {
   float x;
-  if constexpr (F8) x = (row[e] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
+  if constexpr (F8) x = Codes<T>::one((uint8_t)row[e], scale);
   else if constexpr (Elem<T>::kBytes == 2) x = bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(row + 2 * e));
   else x = *reinterpret_cast<const float*>(row + 4 * e);
   return fabsf(x) < __builtin_inff() ? 0.0f : x;
@@ -430,14 +435,15 @@ __device__ inline float not_finite(const char* row, int e) {
 
 // Whether a held row of V is finite.
 template <typename T, int D, bool F8>
-__device__ inline bool finite_row(const char* row) {
+__device__ inline bool finite_row(const char* row, float scale) {
   bool fine = true;
 #pragma unroll 1
   for (int i = 0; i < D * (F8 ? 1 : Elem<T>::kBytes) / 16; ++i) {
     const uint4 w = *reinterpret_cast<const uint4*>(row + 16 * i);
     if constexpr (F8) {
       const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-      for (int j = 0; j < 16; ++j) fine = fine && ((u[j >> 2] >> (8 * (j & 3))) & 0x7f) != 0x7f;
+#pragma unroll
+      for (int j = 0; j < 4; j += Codes<T>::kWords) fine = fine && finite16<T>(Codes<T>::decode(u + j, scale));
     } else {
       fine = fine && finite16<T>(w);
     }
@@ -449,7 +455,7 @@ __device__ inline bool finite_row(const char* row) {
 // would bring it to rows that do not attend its key). Where there was such, the
 // units first, first + stride, ... before `last`, of `sub` tiles each, are looked
 // through again after the loop, the masked tiles or all of them, and add(position,
-// row) adds it to the rows that do attend it. Rare, and apart from the loop: inside
+// row, its scale) adds it to the rows that do attend it. Rare, and apart from the loop: inside
 // it, it cost the loop its registers.
 template <typename T, int D, int KT, bool F8, typename Add>
 __device__ inline void bad_rows(const KvItem& a, int first, int last, int stride, int sub, int first_pos, bool all,
@@ -458,12 +464,15 @@ __device__ inline void bad_rows(const KvItem& a, int first, int last, int stride
     const uint64_t ok = present<KT>(a, y, lane);
     if (!all && ok == all_keys<KT>() && y * KT + KT - 1 <= first_pos) continue;  // not masked
     bool fine = true;
-    if ((ok >> lane) & 1) fine = finite_row<T, D, F8>(a.v_row(y * KT + lane));  // a row per lane
+    if ((ok >> lane) & 1) {  // a row per lane
+      const int t = y * KT + lane;
+      fine = finite_row<T, D, F8>(a.v_row(t), F8 ? a.v_row_scale(t) : 1.0f);
+    }
     uint64_t bad = __ballot(!fine);
     while (bad) {
       const int t = y * KT + __builtin_ctzll(bad);
       bad &= bad - 1;
-      add(t, a.v_row(t));
+      add(t, a.v_row(t), F8 ? a.v_row_scale(t) : 1.0f);
     }
   }
 }
@@ -641,13 +650,13 @@ struct WaveRows {
 
   template <bool F8>
   __device__ inline void add_bad(const KvItem& a, int first, int last, int first_pos, int lane) {
-    bad_rows<T, D, KT, F8>(a, first, last, 1, 1, first_pos, false, lane, [&](int t, const char* row) {
+    bad_rows<T, D, KT, F8>(a, first, last, 1, 1, first_pos, false, lane, [&](int t, const char* row, float scale) {
       if (pos < t) return;
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          oacc[dt][v] += not_finite<T, F8>(row, 32 * dt + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3));
+          oacc[dt][v] += not_finite<T, F8>(row, scale, 32 * dt + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3));
           __builtin_amdgcn_sched_barrier(0);
         }
     });
@@ -889,12 +898,12 @@ struct FewRows {
           for (int v = 0; v < 4; ++v)
             if (!(fabsf(oacc[r][dt][v]) < __builtin_inff())) spoilt |= 1u << ((r * NDT + dt) * 4 + v);
     }
-    bad_rows<T, D, 32, F8>(a, first, last, stride, sub, first_pos, __any(spoilt != 0), lane, [&](int t, const char* row) {
+    bad_rows<T, D, 32, F8>(a, first, last, stride, sub, first_pos, __any(spoilt != 0), lane, [&](int t, const char* row, float scale) {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const float x = not_finite<T, F8>(row, 16 * dt + 4 * (lane >> 4) + v);
+          const float x = not_finite<T, F8>(row, scale, 16 * dt + 4 * (lane >> 4) + v);
 #pragma unroll
           for (int r = 0; r < NR; ++r) {
             if (x == 0.0f || pos[r] < t) continue;

@@ -64,6 +64,9 @@ template <> struct Codes<__bf16> {
     return make_uint4(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b),
                       __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d));
   }
+  __device__ static inline float one(uint8_t code, float scale) {
+    return (float)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, scale, false)[0];
+  }
 };
 template <> struct Codes<float> {
   static constexpr int kWords = 1;
@@ -72,6 +75,9 @@ template <> struct Codes<float> {
     const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[0], true);
     return make_uint4(__float_as_uint(a[0] * scale), __float_as_uint(a[1] * scale), __float_as_uint(b[0] * scale),
                       __float_as_uint(b[1] * scale));
+  }
+  __device__ static inline float one(uint8_t code, float scale) {
+    return __builtin_amdgcn_cvt_pk_f32_fp8(code, false)[0] * scale;
   }
 };
 

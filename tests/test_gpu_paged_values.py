@@ -138,3 +138,36 @@ def test_infinities_in_attended_values(dtype, d, heads, ctx, rows, expected):
         cache.v[int(page[t // 32]), t % 32, h, i] = float(Vd[0][t, h, i])
     Q = torch.randn(rows, heads[0], d, generator=gen).to(dtype).cuda()
     _attend_not_finite(cfg, cache, Q, begin, Kd[0], Vd[0], 1 if expected == "one" else rows, "infinities")
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 64)])
+@pytest.mark.parametrize("ctx,rows", [(300, 140), (3000, 3)])
+@pytest.mark.parametrize("expected", ["one", "all"])
+def test_codes_that_stand_for_infinities(dtype, d, ctx, rows, expected):
+    """A pool of the caller's making whose codes and scales stand for 2^128: read
+    back and attended as the infinity that it is in float32, whether a tile is masked."""
+    say(f"[read, attend] infinite codes, {dtype}, d {d}, {rows} rows over {ctx}, {expected}")
+    gen = torch.Generator().manual_seed(44)
+    cfg = _cfg(4, 2, d, dtype)
+    cache = _cache(cfg, 1, -(-ctx // 32), -(-ctx // 32), 32, True, "head")
+    _fill_table(cache, [ctx], gen)
+    Kd, Vd = _context(cfg, cache, [ctx], gen, True)
+    page, begin = cache.page_table[0].cpu(), ctx - rows
+    codes = cache.v.view(torch.uint8)
+    for t, h in ((5, 0), (100, 1), (begin - 2, 0), (begin + rows // 2, 1)):
+        p, o = int(page[t // 32]), t % 32
+        codes[p, o, h] = 0
+        cache.v_scale[p, h, o] = 120 + 127
+        Vd[0][t, h] = 0.0
+        for i, c, v in ((t % 11, 0x78, math.inf), (20 + t % 7, 0xF8, -math.inf), (40, 0x7F, math.nan)):
+            codes[p, o, h, i] = c
+            Vd[0][t, h, i] = v
+    for t, h, i, c, v in ((7, 1, 3, 0x7F, math.nan), (begin + 1, 0, 4, 0xFF, math.nan)):
+        codes[int(page[t // 32]), t % 32, h, i] = c
+        Vd[0][t, h, i] = v
+    out = torch.full((2, ctx, 2, d), 7.0, dtype=dtype, device="cuda")
+    hga.cache_read(cfg, cache, out[0], out[1], _rows([0, ctx]), _rows([0]))
+    got = out[1].double().cpu()
+    assert bool(((got == Vd[0]) | (torch.isnan(got) & torch.isnan(Vd[0]))).all())
+    Q = torch.randn(rows, 4, d, generator=gen).to(dtype).cuda()
+    _attend_not_finite(cfg, cache, Q, begin, Kd[0], Vd[0], 1 if expected == "one" else rows, "infinite codes")
