@@ -489,6 +489,7 @@ hga_status_t hga_attend_gathered_bwd(const hga_config_t* cfg, const void* Q, hga
  *               zeros, and attention leaves its positions out. Pages may be
  *               shared by sequences.
  *   page_size   a power of two in [16, 65536].
+ *   n_seqs      at most 2^30.
  * Formats:
  *   HGA_CACHE_SAME  rows in cfg->dtype, copied;
  *   HGA_CACHE_E4M3  rows in 8 bits (OCP e4m3: 3 bits of mantissa, largest value

@@ -56,6 +56,7 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 constexpr int64_t kMaxTokens = (int64_t)1 << 31;
 constexpr int64_t kMaxStrideBytes = (int64_t)1 << 32;
 constexpr int64_t kMaxTokenBytes = (int64_t)1 << 27;  // token stride inside a cache page
+constexpr int kMaxSeqs = 1 << 30;                     // sequences of a paged cache
 
 hga_status_t check_tensor(const void* p, hga_strides_t s, int eb) {
   if (!p || !aligned16(p)) return HGA_ERR_INVALID_ARG;
@@ -816,6 +817,8 @@ static hga_status_t paged_args(const hga_config_t* cfg, const hga_paged_cache_t*
   if (e4m3 && (!c->k_scale || !c->v_scale)) return HGA_ERR_INVALID_ARG;
   if (c->n_seqs < 1 || c->table_cap < 1 || c->n_pages < 1) return HGA_ERR_INVALID_ARG;
   if (c->table_cap > kMaxTokens || c->n_pages >= kMaxTokens) return HGA_ERR_UNSUPPORTED;
+  // 32-bit indexes pass the last of n_seqs + 1 entries by up to a workgroup
+  if (c->n_seqs > kMaxSeqs) return HGA_ERR_UNSUPPORTED;
   if (c->page_size < 1) return HGA_ERR_INVALID_ARG;
   if (c->page_size < 16 || c->page_size > 65536 || log2_exact(c->page_size) < 0) return HGA_ERR_UNSUPPORTED;
   const int eb = e4m3 ? 1 : elem_bytes(cfg);
