@@ -482,7 +482,8 @@ hga_status_t hga_attend_gathered_bwd(const hga_config_t* cfg, const void* Q, hga
  *               elements (strides ks / vs, in elements of the format; 16-byte
  *               aligned rows; any order of the axes). Page and head strides
  *               below 2^32 bytes, token strides below 2^27 bytes.
- *   k_scale, v_scale  HGA_CACHE_E4M3: uint8 [n_pages][Hkv][page_size]; else unused.
+ *   k_scale, v_scale  HGA_CACHE_E4M3: uint8 [n_pages][Hkv][page_size], Hkv *
+ *               page_size below 2^32; else unused.
  *   page_table  int32 [n_seqs][table_cap]. An entry outside [0, n_pages) is an
  *               absent page, as is a position outside the table (or from 2^31 - 128
  *               on): rows written there are dropped, rows read from there are

@@ -821,6 +821,8 @@ static hga_status_t paged_args(const hga_config_t* cfg, const hga_paged_cache_t*
   if (c->n_seqs > kMaxSeqs) return HGA_ERR_UNSUPPORTED;
   if (c->page_size < 1) return HGA_ERR_INVALID_ARG;
   if (c->page_size < 16 || c->page_size > 65536 || log2_exact(c->page_size) < 0) return HGA_ERR_UNSUPPORTED;
+  // a page's scales, a stride of 32 bits in the attention
+  if (e4m3 && (int64_t)cfg->n_kv_heads * c->page_size >= kMaxStrideBytes) return HGA_ERR_UNSUPPORTED;
   const int eb = e4m3 ? 1 : elem_bytes(cfg);
   const hga_page_strides_t st[2] = {c->ks, c->vs};
   for (const hga_page_strides_t& x : st) {
