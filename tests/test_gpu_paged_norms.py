@@ -107,3 +107,29 @@ def test_shares_of_hundreds_of_tiles(d, rows, e4m3):
     begin = [ctx - rows - 37 * s for s in range(S)]
     _check(cfg, cache, Q, [rows * s for s in range(S + 1)], begin, [Kd[0]] * S, [Vd[0]] * S, rows, "long shares",
            only=(0, 7, 40, 63))
+
+
+@pytest.mark.parametrize("d,hq,hkv,rows", [(128, 8, 2, [1] * 9), (128, 4, 4, [16, 9, 1, 12]), (64, 8, 2, [1, 4, 2, 4]),
+                                           (64, 8, 1, [8, 5, 1, 7]), (128, 8, 2, [300, 1, 4, 3, 2, 4, 4]),
+                                           (64, 8, 2, [140, 1, 4, 3, 2, 4, 4])])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_few_rows_have_p_as_a_pair(d, hq, hkv, rows, e4m3):
+    """Over the rows of the forms of 16 and 32 (alone, or beside a chunk) the error is
+    that of rounding O."""
+    say(f"[attend] pairs, {hq}/{hkv} heads, d {d}, rows {rows}, e4m3 {e4m3}")
+    gen = torch.Generator().manual_seed(54)
+    cfg = _cfg(hq, hkv, d, BF)
+    ctx = [700 + 150 * s for s in range(len(rows))]
+    cache = _cache(cfg, len(rows), 30, sum(-(-c // 64) for c in ctx), 64, e4m3, "head", fill=0xFF)
+    _fill_table(cache, ctx, gen)
+    Kd, Vd = _context(cfg, cache, ctx, gen, e4m3)
+    first = [0]
+    for r in rows:
+        first.append(first[-1] + r)
+    Q = torch.randn(first[-1], hq, d, generator=gen).to(BF).cuda()
+    got = _check(cfg, cache, Q, first, [c - r for c, r in zip(ctx, rows)], Kd, Vd, max(rows), "pairs")
+    few = [(o, z) for o, z, pair in got if pair]
+    assert len(few) >= len(rows) - 1
+    ratio = pn.rounding_ratio(torch.cat([o for o, _ in few]), torch.cat([z for _, z in few]))
+    say(f"   {ratio:.4f} of the rounding's error")
+    assert ratio < 1.1

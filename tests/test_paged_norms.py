@@ -86,3 +86,14 @@ def test_dropped_keys_of_a_long_context_are_seen(ctx, rows, hq, hkv, d, dtype):
         drop = slice(ctx // 3, ctx // 3 + n)
         eo, ez = pn.excess(*_like_the_kernel(Q, K, V, ok, pos, 24 if dtype == F32 else 8, drop), ref, dtype == BF, False)
         assert ez > 1, (n, ez)
+
+
+@pytest.mark.parametrize("ctx,rows,hq,hkv,d,dtype", [s for s in SIZES if s[5] == BF])
+def test_a_weight_of_too_few_bits_is_seen(ctx, rows, hq, hkv, d, dtype):
+    """Over some rows: P as one bf16 value where it should be a pair, and P of five
+    significant bits where it should be one."""
+    x = _inputs(ctx, max(rows, 12 if ctx > 10000 else 24), hq, hkv, d, dtype, seed=2)
+    ref = pn.reference(*x, 1 / math.sqrt(d))
+    assert pn.rounding_ratio(_like_the_kernel(*x, 16)[0], ref[0]) < 1.1
+    assert pn.rounding_ratio(_like_the_kernel(*x, 8)[0], ref[0]) > 1.1
+    assert pn.excess(*_like_the_kernel(*x, 5), ref, True, False)[0] > 1
