@@ -918,31 +918,49 @@ static size_t paged_ws(const hga_config_t* c, int64_t n_rows, PagedForm form) {
   return hga::paged_workgroups(form) * sizeof(int4) + rows * (c->head_dim + 2) * sizeof(float);  // a multiple of 16
 }
 // The forms a call runs, by the most folded rows that a sequence of it has: 16 at
-// a time where that is all; 32 at a time up to a limit; else 256 at a time.
-// Beside the larger ones the sequences of at most 16 have the form of 16 (generation
-// beside a prompt's chunk), unless all have at most 32: a launch more costs more
-// than it gives there. A form alone takes whatever there is.
-// The form of 32 reads K and V once per 32 rows, but leaves no wave without rows
-// (us, 16 sequences of 8,192 keys; 32 against 256 at a time):
-//   d = 128, bf16, 8 kv heads: 32 rows 136 against 118, 48 177 against 116: never;
-//   d = 64, bf16, 2 kv heads: 32 rows 28 against 31, 64 28 against 33, 96 47
-//   against 34; float32: 32 rows 47 against 123, 64 65 against 125, 308 234 against
-//   348, but with 1,500 keys in 8 bits 50 against 36: to 64.
-static int paged_forms(const hga_config_t* c, int64_t n_seqs, int64_t n_rows, int64_t max_rows,
+// a time where that is all; 32 at a time up to a limit; else 256 at a time. In a
+// batch of several sequences those of at most 16 have the form of 16 beside the
+// larger ones (generation beside a prompt's chunk): with d = 64 where the most is over
+// 32, with d = 128 where it is over 16. A form alone takes whatever there is.
+// The form of 32 reads K and V once per 32 rows, but leaves no wave without rows,
+// and its waves take different keys, so it needs many of them (us; S sequences):
+//   d = 128: not built. Twice the form of 16 against that of 256, 32 rows of 8 kv
+//   heads: bf16 pool S = 1 of 32,768 keys 55 against 39, 16 of 8,192 108 against 118,
+//   64 of 4,096 368 against 205; 8 bits 41 against 37, 76 against 99, 204 against 177.
+//   d = 64, bf16, 2 kv heads, 16 of 8,192: 32 rows 28 against 31, 64 28 against 33, 96
+//   47 against 34.
+//   float32: by the rows of K and V that the call may read, its sequences' by kv heads
+//   by positions of the table. Of 392 points (S 1 to 64, 400 to 65,536 keys, 8 or 2 kv
+//   heads, both formats, 68 to 4,096 rows) the form of 32 was the faster by up to 1.64
+//   (68 rows of 8 heads, 16 of 8,192 in 8 bits, 271 against 445) with up to 1,024 rows
+//   and 20,000 of K, the slower by up to 1.95 with fewer (96 rows of 8 heads, one of 400
+//   in 8 bits, 39 against 20), and as fast or slower from 1,280 rows on. This rule is
+//   within a tenth of the better one at 365 of them; 256 at a time always, at 209.
+static int few_limit(const hga_config_t* c, double kv_rows) {
+  if (c->head_dim != 64) return 16;
+  return c->dtype == HGA_F32 && kv_rows >= 20000 ? 1024 : 64;
+}
+static int paged_forms(const hga_config_t* c, int64_t n_seqs, int64_t positions, int64_t n_rows, int64_t max_rows,
                        PagedForm (&forms)[2]) {
   const int64_t rows = max_rows < n_rows ? max_rows : n_rows, folded = rows * (c->n_q_heads / c->n_kv_heads);
-  const int limit = c->head_dim == 64 ? 64 : 16;
+  const int64_t seqs = n_seqs < n_rows ? n_seqs : n_rows;  // the others have no rows
+  const int limit = few_limit(c, (double)seqs * positions * c->n_kv_heads);
   forms[0] = folded <= 16 ? PagedForm::kFew16 : folded <= limit ? PagedForm::kFew32 : PagedForm::kTile;
   forms[1] = PagedForm::kFew16;
-  return n_seqs > 1 && folded > (limit > 32 ? 32 : 16) ? 2 : 1;
+  return n_seqs > 1 && folded > (c->head_dim == 64 ? 32 : 16) ? 2 : 1;
 }
 
 size_t hga_paged_workspace_size(const hga_config_t* cfg, int64_t n_rows, int64_t max_rows) {
   if (check_cfg(cfg) != HGA_OK || n_rows < 1 || n_rows >= kMaxTokens || max_rows < 1) return 0;
-  PagedForm forms[2];
-  size_t need = 0;
-  for (int i = 0, n = paged_forms(cfg, 2, n_rows, max_rows, forms); i < n; ++i) need += paged_ws(cfg, n_rows, forms[i]);
-  return need;
+  size_t most = 0;
+  for (int64_t positions : {(int64_t)1, kMaxTokens}) {  // of few and of many: the table is not known
+    PagedForm forms[2];
+    size_t need = 0;
+    for (int i = 0, n = paged_forms(cfg, 2, positions, n_rows, max_rows, forms); i < n; ++i)
+      need += paged_ws(cfg, n_rows, forms[i]);
+    most = need > most ? need : most;
+  }
+  return most;
 }
 
 hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache_t* cache, const void* Q,
@@ -967,7 +985,8 @@ hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache
   a.scale_log2 = eff_scale(cfg) * 1.4426950408889634f;
   PagedForm forms[2];
   hga::PagedAttnArgs args[2];
-  const int n_forms = paged_forms(cfg, cache->n_seqs, n_rows, max_rows, forms), few_rows = 16 / G;
+  const int n_forms = paged_forms(cfg, cache->n_seqs, cache->table_cap << a.p.page_shift, n_rows, max_rows, forms);
+  const int few_rows = 16 / G;
   char* ws = static_cast<char*>(workspace);
   for (int i = 0; i < n_forms; ++i) {
     a.min_rows = n_forms == 2 && i == 0 ? few_rows + 1 : 1;
