@@ -562,7 +562,9 @@ hga_status_t hga_cache_read(const hga_config_t* cfg, const hga_paged_cache_t* ca
  * sequence `seq` read from the cache: the routed path over a paged, 8-bit
  * history. Kc, Vc, r_cap and the order of the rows as there;
  * hga_attend_gathered_fwd and hga_attend_gathered_bwd read them. Rows of absent
- * pages are zeros.
+ * pages are zeros, and attention over the gathered rows counts them, as keys of
+ * score 0 (hga_attend_paged_fwd leaves them out): the selection and the windows
+ * of a sequence that is routed have to lie in present pages.
  */
 hga_status_t hga_gather_paged(const hga_config_t* cfg, const hga_paged_cache_t* cache, int64_t seq,
                               int64_t q_begin, int64_t n_q,
@@ -577,7 +579,7 @@ hga_status_t hga_gather_paged(const hga_config_t* cfg, const hga_paged_cache_t* 
  * chunks of a prompt, and both in one batch. Keys after a row never enter its
  * result, infinities and NaN among them. An infinity in V makes the elements of
  * the rows that attend it infinite, or NaN: where it meets NaN or an infinity of
- * the other sign, or has a weight of zero in float32.
+ * the other sign, or has a weight below 2^-126.
  *
  *   Q          rows [0, n_rows) of cfg->dtype, strides qs.
  *   O          rows [0, n_rows) of cfg->dtype, strides os (bf16 rounded to nearest even).

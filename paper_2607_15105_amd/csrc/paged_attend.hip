@@ -868,19 +868,17 @@ struct FewRows {
     }
   }
 
-  // bf16: whether the products left O finite. An infinity of V is one by P's high half,
-  // but NaN by a low half of zero, or by one of the other sign.
+  // bf16: whether the products left O finite, by its sum (a sum that overflows only has
+  // its tiles looked at). An infinity of V is one by P's high half, but NaN by a low half
+  // of zero, or by one of the other sign.
   __device__ __forceinline__ bool finite() const {
-    float z = 0.0f;
-    if constexpr (EB == 2) {
+    if constexpr (EB == 4) return true;
+    f32x4 z = f32x4{};
 #pragma unroll
-      for (int r = 0; r < NR; ++r)
+    for (int r = 0; r < NR; ++r)
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) z = fmaf(oacc[r][dt][v], 0.0f, z);
-    }
-    return !__any(z != 0.0f);
+      for (int dt = 0; dt < NDT; ++dt) z += oacc[r][dt];
+    return !__any(!(fabsf((z[0] + z[1]) + (z[2] + z[3])) < __builtin_inff()));
   }
 
   // Adds what masked tiles left out, and puts it in the place of what the products made
