@@ -1000,6 +1000,8 @@ hga_status_t hga_attend_paged_fwd(const hga_config_t* cfg, const hga_paged_cache
   }
   // Few rows of few contexts may have 32 parts each or more, which four half waves
   // join (64 parts 12 -> 7 us; where they are eight, the further workgroups cost 4 us).
+  // Contexts are counted by the cache's sequences, idle ones among them: their lengths
+  // are on the device.
   const bool many = hga::paged_workgroups(forms[0]) >= 32ll * cache->n_seqs * cfg->n_kv_heads;
   const int split = many && n_forms == 1 && args[0].slot_rows <= 32 ? 4 : 1;
   if (hga::launch_attend_paged(args, forms, n_forms, split, cache->format == HGA_CACHE_E4M3, cfg->dtype == HGA_BF16,

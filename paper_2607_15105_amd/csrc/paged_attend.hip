@@ -926,8 +926,8 @@ struct FewRows {
 // although the matrix cores have time to spare: it is the instructions beside
 // them that count (with 32 rows, 64 ragged contexts in 8 bits took 180 us, with 16
 // and P rounded 175). What bounds it: the memory where contexts are long (eight
-// of 131K in 8 bits 381 us, 5.7 TB/s), the starts and ends of items beside it where
-// they are not (64 of 1K to 16K 178 us, 4.9 TB/s), and a chain of round trips for
+// of 131K in 8 bits 380 us, 5.7 TB/s), the starts and ends of items beside it where
+// they are not (64 of 1K to 16K 180 us, 4.8 TB/s), and a chain of round trips for
 // one short context (2K: 10 us, of which 2 are the launch, 1.5 the share, 5 the tile).
 template <typename T, int D, bool F8, int NR>
 __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs) {
@@ -1059,10 +1059,11 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs) {
 //
 // What bounds it: 2,048 rows of 32 heads at the end of 32K (bf16 rows) take
 // 0.99 to 1.10 ms by the card, 0.97 to 1.07 PFLOP/s (0.87 ms on zeros: the clock
-// falls under the power of products of real values). A product takes 34 cycles
-// of a SIMD and hides about four vector instructions; 32 keys of a wave have 16
-// products, 16 exponentials and some 60 others. Without the staging of tiles it took
-// 0.71 ms on zeros. Longer operand queues, wave priorities, staggered waves and
+// falls under the power of products of real values, to 1.7 GHz where calls run one at
+// a time). A product takes 32 cycles of a matrix core, which is busy half of the
+// time, and there are 5.2 vector instructions beside each: 32 keys of a wave have 16
+// products, 16 exponentials and some 70 others. 76 of 100 reads of keys are L2
+// hits. Without the staging of tiles it took 0.71 ms on zeros. Longer operand queues, wave priorities, staggered waves and
 // the exponentials spread over both kinds of product changed it by 1% at most;
 // one phase after the other, 1.10 ms.
 template <typename T, int D, bool F8>
