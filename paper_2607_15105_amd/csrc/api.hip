@@ -936,6 +936,8 @@ static size_t paged_ws(const hga_config_t* c, int64_t n_rows, PagedForm form) {
 //   and 20,000 of K, the slower by up to 1.95 with fewer (96 rows of 8 heads, one of 400
 //   in 8 bits, 39 against 20), and as fast or slower from 1,280 rows on. This rule is
 //   within a tenth of the better one at 365 of them; 256 at a time always, at 209.
+//   (Lengths are on the device: short contexts in a table of many positions are taken
+//   for long ones.)
 static int few_limit(const hga_config_t* c, double kv_rows) {
   if (c->head_dim != 64) return 16;
   return c->dtype == HGA_F32 && kv_rows >= 20000 ? 1024 : 64;

@@ -455,8 +455,8 @@ __device__ inline bool finite_row(const char* row, float scale) {
 // would bring it to rows that do not attend its key). Where there was such, the
 // units first, first + stride, ... before `last`, of `sub` tiles each, are looked
 // through again after the loop, the masked tiles or all of them, and add(position,
-// row, its scale) adds it to the rows that do attend it. Rare, and apart from the loop: inside
-// it, it cost the loop its registers.
+// row, its scale) adds it to the rows that do attend it. Rare, and apart from the
+// loop: inside it, it cost the loop its registers.
 template <typename T, int D, int KT, bool F8, typename Add>
 __device__ inline void bad_rows(const KvItem& a, int first, int last, int stride, int sub, int first_pos, bool all,
                                 int lane, Add&& add) {
@@ -896,7 +896,8 @@ struct FewRows {
           for (int v = 0; v < 4; ++v)
             if (!(fabsf(oacc[r][dt][v]) < __builtin_inff())) spoilt |= 1u << ((r * NDT + dt) * 4 + v);
     }
-    bad_rows<T, D, 32, F8>(a, first, last, stride, sub, first_pos, __any(spoilt != 0), lane, [&](int t, const char* row, float scale) {
+    const bool all = __any(spoilt != 0);
+    bad_rows<T, D, 32, F8>(a, first, last, stride, sub, first_pos, all, lane, [&](int t, const char* row, float scale) {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
@@ -1063,9 +1064,9 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedAttnArgs) {
 // a time). A product takes 32 cycles of a matrix core, which is busy half of the
 // time, and there are 5.2 vector instructions beside each: 32 keys of a wave have 16
 // products, 16 exponentials and some 70 others. 76 of 100 reads of keys are L2
-// hits. Without the staging of tiles it took 0.71 ms on zeros. Longer operand queues, wave priorities, staggered waves and
-// the exponentials spread over both kinds of product changed it by 1% at most;
-// one phase after the other, 1.10 ms.
+// hits. Without the staging of tiles it took 0.71 ms on zeros. Longer operand
+// queues, wave priorities, staggered waves and the exponentials spread over both
+// kinds of product changed it by 1% at most; one phase after the other, 1.10 ms.
 template <typename T, int D, bool F8>
 __global__ __launch_bounds__(512) void paged_tile_kernel(PagedAttnArgs) {
   constexpr int KT = 1 << kPagedTileKeys, NW = 8;
